@@ -354,6 +354,129 @@ int halp_debug_read_bandwidth(const void* p, int64_t bytes, uint32_t* out, void*
 int halp_debug_step_latency(int32_t waves, int64_t steps, int32_t blocks, uint32_t* out,
                             void* stream);
 
+/* ---- 4-bit microscaled matrices ------------------------------------------------------------
+ *
+ * A second low-precision representation beside (delta_d, b): floating point in 4 bits with a scale
+ * for every 32 values of a row, and products of matrices held in it on the matrix cores (margins
+ * X W^T of models with many outputs, and, with operands quantized along the other axis, the
+ * gradients of such a product).  None of these calls needs a handle or allocates memory.
+ *
+ * A block is 32 consecutive values of a row.  It has one scale byte s, 2^(s - 127), and a value is
+ * a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7).  s is the smallest with
+ * max |x| <= 6 * 2^(s - 127), s >= 0: no value is clamped.  A block that holds an infinity or a NaN
+ * gets s = 255 and reads as NaN throughout.  A row is stored in groups of 128 values: 64 bytes of
+ * codes (value 2 i of the row in the low half of byte i) and 4 scale bytes; the places behind its
+ * last column, up to a whole group, are part of the row and hold codes and scales of zero
+ * (halp_mx4_quantize writes them).                                                             */
+
+/* value types of the operators from here on */
+#define HALP_TYPE_F32 0
+#define HALP_TYPE_BF16 1
+#define HALP_TYPE_F16 2
+
+#define HALP_ROUND_NEAREST 0    /* ties to the even code                                       */
+#define HALP_ROUND_STOCHASTIC 1 /* up or down at random, unbiased to 1/512 of a step           */
+
+typedef struct {
+  void* codes;    /* DEVICE [rows][ldc], 16-byte aligned                                        */
+  int64_t ldc;    /* bytes from row to row, a multiple of 16, >= 64 ceil(cols / 128)           */
+  uint8_t* scales; /* DEVICE [rows][lds], 4-byte aligned                                        */
+  int64_t lds;    /* bytes from row to row, a multiple of 4, >= 4 ceil(cols / 128)             */
+  int64_t rows, cols; /* 0 <= rows, cols < 2^31                                                */
+} halp_mx4;
+
+/* x (DEVICE, rows of ldx >= cols elements of `type`, any alignment of its type) into MX4 with x
+ * read once: q ([rows][cols], blocks along x's rows), qt ([cols][rows], the transpose, blocks
+ * along x's columns), or both; either may be NULL.  rounding HALP_ROUND_STOCHASTIC: with r = 8
+ * bits of the stream of `seed` and `epoch` (0 <= epoch < 2^32), a value is rounded up where the
+ * fraction of |x| / step is at least (511 - 2 r) / 512; element (i, j) of a form takes byte j % 16
+ * of block i * ceil(cols / 16) + j / 16 of purpose 6 (q) or 7 (qt, in its own rows and columns).
+ * x, q and qt must not overlap.                                                               */
+int halp_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, const halp_mx4* q,
+                      const halp_mx4* qt, int32_t rounding, uint64_t seed, int64_t epoch, void* stream);
+
+/* The values that q stands for, into out (DEVICE, [rows][ldo], ldo >= cols, elements of `type`):
+ * exact in fp32 and bf16 (below 2^-126: rounded to the type); fp16 rounds, and overflows to
+ * infinity.                                                                                   */
+int halp_mx4_dequantize(const halp_mx4* q, void* out, int32_t type, int64_t ldo, void* stream);
+
+/* c[M][N] = a[M][K] b[N][K]^T, and added to c where accumulate is 1 (fp32 only); M = a->rows,
+ * N = b->rows, K = a->cols = b->cols, rows of c ldc >= N elements of `type`.  Products of values
+ * are exact; sums are kept in fp32.  With dY a gradient of the product in a and b as its operands
+ * were before quantization (rounding taken as the identity), the gradients are products too:
+ * dA = dY B of Q(dY) and the qt form of b, dB = dY^T A of the qt forms of dY and a.
+ * K = 0 gives zeros.  workspace (DEVICE, 16-byte aligned, may be NULL): with at least
+ * halp_mx4_product_workspace bytes, products with few tiles and a long K are cut along K and their parts joined in a
+ * fixed order; without it the same products run uncut and end in another rounding.  Calls that
+ * overlap in time must not share it.  c must not overlap the operands or the workspace.        */
+int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type, int64_t ldc, int32_t accumulate,
+                     void* workspace, int64_t workspace_bytes, void* stream);
+int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes); /* on the current device */
+
+/* y[M][N] = Q(x)[M][K] w[N][K]^T for 0 <= M <= 16 rows of x in `xtype`, quantized to the nearest on the
+ * way (the values halp_mx4_quantize gives): a served token's product in one launch.  Larger M:
+ * HALP_ERR_UNSUPPORTED, quantize x and take halp_mx4_product.                                  */
+int halp_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, const halp_mx4* w, void* y,
+                         int32_t ytype, int64_t ldy, void* stream);
+
+/* ---- AdamW over many tensors ----------------------------------------------------------------
+ *
+ * The first-order optimizer beside Algorithms 1, 2 and 4 for models with many tensors, one launch
+ * for all of them: with s the gradient scale and t the step (from 1),
+ *   g' = g s;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr weight_decay) - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32.  States are fp32, or take 8 bits an element and 1 / 16 byte of scales: blocks of 32 elements
+ * with scales 2^(s - 127); m with a sign, 4 exponent bits (bias 7) and 3 mantissa bits, largest
+ * 448; v with 5 exponent bits (bias 15) and 3 mantissa bits, largest 61440; s as small as
+ * the largest of the block allows.  They are rounded stochastically, so that the small
+ * changes that beta2 makes are not lost: element e of tensor i takes word e % 4 of block e / 4 of
+ * purpose 8 of the stream of seed + i at epoch t, the low half for m and the high half for v;
+ * p is updated from m and v before that rounding.  A block whose m (or v) is not finite
+ * gets s = 255 and reads as NaN.                                                              */
+typedef struct halp_adamw halp_adamw; /* opaque, library-owned */
+
+typedef struct { /* DEVICE pointers of one tensor of n contiguous elements (n >= 0) */
+  float* p;         /* in/out                                                                  */
+  const void* g;    /* in, grad_type                                                           */
+  void* m;          /* in/out  32 bits: float [n]; 8 bits: codes [n]                           */
+  void* v;          /* in/out  likewise                                                        */
+  uint8_t* m_scale; /* in/out  8 bits: [ceil(n / 32)]; 32 bits: NULL                           */
+  uint8_t* v_scale; /* in/out  likewise                                                        */
+  void* copy;       /* out     p in copy_type, or NULL                                         */
+  int64_t n;
+} halp_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* lr >= 0, 0 <= beta < 1, eps > 0, weight_decay >= 0 */
+  int64_t step;           /* t, 1 <= t < 2^32                                                  */
+  const int64_t* step_at; /* DEVICE, or NULL: t is read there instead (a step captured into a
+                             graph; the caller counts it up).  A t out of range skips the step */
+  const float* lr_at;     /* DEVICE, or NULL: lr is read there instead                         */
+  const float* grad_scale; /* DEVICE, or NULL for 1: s.  Where it is not finite the step is
+                             skipped: every tensor is left as it was                           */
+} halp_adamw_args;
+
+/* The plan of a list of tensors: copies the list to the current device (the structs need not
+ * outlive the call, the tensors do).  Tensors must not overlap; count >= 1.  state_bits 8 or 32.
+ * Every pointer is aligned to its element.  Tensors whose p, g, m, v and copy are aligned to
+ * four elements run fastest.                                                                 */
+int halp_adamw_create(halp_adamw** out, const halp_adamw_tensor* tensors, int64_t count, int32_t state_bits,
+                      int32_t grad_type, int32_t copy_type, uint64_t seed);
+int halp_adamw_destroy(halp_adamw* h);
+
+/* One step of every tensor.  A handle keeps nothing between steps but its list.               */
+int halp_adamw_step(halp_adamw* h, const halp_adamw_args* args, void* stream);
+
+/* out[0] = the 2-norm of all gradients, out[1] = min(1, max_norm / out[0]), the grad_scale that
+ * clips to it (1 for a norm of 0; NaN where the norm is not finite, so that the step is skipped).
+ * Sums in 64 bits, joined in a fixed order, through workspace of the handle: calls on one handle that
+ * overlap in time race.                                                                       */
+int halp_adamw_grad_norm(halp_adamw* h, double max_norm, float* out, void* stream);
+
+/* The values of 8-bit states of n elements in fp32, for checkpoints and for looking at them.   */
+int halp_adamw_read_moments(const uint8_t* m, const uint8_t* m_scale, const uint8_t* v, const uint8_t* v_scale,
+                            int64_t n, float* m_out, float* v_out, void* stream);
+
 const char* halp_strerror(int code);
 /* Text of the last HIP runtime failure seen by this thread inside the library
  * (which call, and HIP's message); empty if there was none.                            */

@@ -20,6 +20,8 @@ OPT_GRADIENT_FP32 = 12
 ERR_NULL, ERR_INVALID, ERR_UNSUPPORTED, ERR_NOT_BOUND, ERR_HIP, ERR_ALIGN = -1, -2, -3, -4, -5, -6
 ERR_TOO_LARGE = -7
 ERR_EXCHANGE_TIMEOUT = -8
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
 STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = [
@@ -28,7 +30,10 @@ EXPORTS = [
     "halp_quantize_data",
     "halp_full_gradient", "halp_full_gradient_static", "halp_recenter", "halp_inner_loop", "halp_epoch",
     "halp_inner_loop_trace", "halp_get_stats", "halp_debug_stream_words",
-    "halp_debug_zround_bits", "halp_debug_read_bandwidth", "halp_debug_step_latency", "halp_strerror", "halp_last_error_detail", "halp_version",
+    "halp_debug_zround_bits", "halp_debug_read_bandwidth", "halp_debug_step_latency",
+    "halp_mx4_quantize", "halp_mx4_dequantize", "halp_mx4_product", "halp_mx4_product_workspace", "halp_mx4_row_product",
+    "halp_adamw_create", "halp_adamw_destroy", "halp_adamw_step", "halp_adamw_grad_norm", "halp_adamw_read_moments",
+    "halp_strerror", "halp_last_error_detail", "halp_version",
 ]
 
 
@@ -67,6 +72,22 @@ class Stats(C.Structure):
     ]
 
 
+class Mx4Struct(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64),
+                ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64)]
+
+
+class AdamWArgs(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64), ("step_at", C.c_void_p), ("lr_at", C.c_void_p),
+                ("grad_scale", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -100,6 +121,17 @@ def lib():
         L.halp_debug_zround_bits.argtypes = [u64, u32, u64, i32, i32, i32, vp, vp]
         L.halp_debug_read_bandwidth.argtypes = [vp, i64, vp, vp]
         L.halp_debug_step_latency.argtypes = [i32, i64, i32, vp, vp]
+        mx = C.POINTER(Mx4Struct)
+        L.halp_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, mx, mx, i32, u64, i64, vp]
+        L.halp_mx4_dequantize.argtypes = [mx, vp, i32, i64, vp]
+        L.halp_mx4_product.argtypes = [mx, mx, vp, i32, i64, i32, vp, i64, vp]
+        L.halp_mx4_product_workspace.argtypes = [i64, i64, i64, C.POINTER(i64)]
+        L.halp_mx4_row_product.argtypes = [vp, i32, i64, i64, mx, vp, i32, i64, vp]
+        L.halp_adamw_create.argtypes = [C.POINTER(vp), C.POINTER(AdamWTensor), i64, i32, i32, i32, u64]
+        L.halp_adamw_destroy.argtypes = [vp]
+        L.halp_adamw_step.argtypes = [vp, C.POINTER(AdamWArgs), vp]
+        L.halp_adamw_grad_norm.argtypes = [vp, C.c_double, vp, vp]
+        L.halp_adamw_read_moments.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp]
         for name in EXPORTS:
             getattr(L, name).restype = C.c_int
         L.halp_strerror.restype = C.c_char_p
@@ -288,3 +320,197 @@ def debug_step_latency(waves, steps, blocks, out=None, stream=None):
     _check(lib().halp_debug_step_latency(waves, steps, blocks, _ptr(out), _stream(stream)),
            "halp_debug_step_latency")
     return out
+
+
+# ---- operators without a handle: 4-bit microscaled matrices, AdamW ---------------------------
+
+_TYPES = {"torch.float32": TYPE_F32, "torch.bfloat16": TYPE_BF16, "torch.float16": TYPE_F16}
+
+
+def _type(t, what):
+    code = _TYPES.get(str(t.dtype))
+    if code is None:
+        raise ValueError(f"{what}: float32, bfloat16 or float16 expected, not {t.dtype}")
+    return code
+
+
+def _matrix(t, what, shape=None):
+    """A 2-D tensor with unit stride along its rows; returns its row stride."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a 2-D tensor with unit stride along its rows expected")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, not {tuple(t.shape)}")
+    # the stride of a single row is whatever torch has it be
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _on(stream, *tensors):
+    """The device the tensors share, made current for the call, and the stream: its current one unless given."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    if dev.type != "cuda":
+        raise ValueError(f"GPU tensors expected, not {dev}")
+    return torch.cuda.device(dev), C.c_void_p(torch.cuda.current_stream(dev).cuda_stream if stream is None else int(stream))
+
+
+class Mx4:
+    """A matrix in 4-bit microscaled form: codes uint8 [rows, >= 64 groups], scales uint8 [rows, >= 4 groups],
+    groups = ceil(cols / 128)."""
+
+    def __init__(self, codes, scales, cols):
+        if str(codes.dtype) != "torch.uint8" or str(scales.dtype) != "torch.uint8":
+            raise ValueError("codes and scales are uint8 tensors")
+        groups = (cols + 127) // 128
+        ldc, lds = _matrix(codes, "codes"), _matrix(scales, "scales")
+        if codes.shape[0] != scales.shape[0] or codes.shape[1] < 64 * groups or scales.shape[1] < 4 * groups:
+            raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not hold rows of {cols} columns")
+        if codes.device != scales.device:
+            raise ValueError("codes and scales are on two devices")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, codes.shape[0], cols
+        # a single row has no stride to speak of: whole groups
+        self.c = Mx4Struct(codes.data_ptr(), ldc if self.rows > 1 else 64 * groups, scales.data_ptr(),
+                           lds if self.rows > 1 else 4 * groups, self.rows, cols)
+
+
+def mx4_empty(rows, cols, device="cuda"):
+    """Allocates an Mx4 whose contents are not set."""
+    import torch
+    groups = (cols + 127) // 128
+    return Mx4(torch.empty((rows, 64 * groups), dtype=torch.uint8, device=device),
+               torch.empty((rows, 4 * groups), dtype=torch.uint8, device=device), cols)
+
+
+def mx4_quantize(x, q=None, qt=None, rounding=ROUND_NEAREST, seed=0, epoch=0, stream=None):
+    """x [rows, cols] into q (Mx4 of its rows) and qt (Mx4 of its transpose), whichever are given."""
+    ldx = _matrix(x, "x")
+    given = [t for m in (q, qt) if m is not None for t in (m.codes, m.scales)]
+    dev, s = _on(stream, x, *given)
+    with dev:
+        _check(lib().halp_mx4_quantize(_ptr(x), _type(x, "x"), x.shape[0], x.shape[1], ldx,
+                                       None if q is None else C.byref(q.c), None if qt is None else C.byref(qt.c),
+                                       rounding, seed & (2 ** 64 - 1), epoch, s), "halp_mx4_quantize")
+
+
+def mx4_dequantize(q, out, stream=None):
+    """The values of q into out [rows, cols]."""
+    ldo = _matrix(out, "out", (q.rows, q.cols))
+    dev, s = _on(stream, out, q.codes)
+    with dev:
+        _check(lib().halp_mx4_dequantize(C.byref(q.c), _ptr(out), _type(out, "out"), ldo, s), "halp_mx4_dequantize")
+
+
+def mx4_product_workspace(M, N, K):
+    """Bytes of workspace with which mx4_product can cut K, on the current device."""
+    n = C.c_int64()
+    _check(lib().halp_mx4_product_workspace(M, N, K, C.byref(n)), "halp_mx4_product_workspace")
+    return n.value
+
+
+def mx4_product(a, b, out, accumulate=False, workspace=None, stream=None):
+    """out [M, N] = a [M, K] b [N, K]^T, added to out where accumulate is set; workspace: a uint8 tensor or None."""
+    ldc = _matrix(out, "out", (a.rows, b.rows))
+    dev, s = _on(stream, out, a.codes, b.codes, workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor expected")
+    with dev:
+        _check(lib().halp_mx4_product(C.byref(a.c), C.byref(b.c), _ptr(out), _type(out, "out"), ldc, int(bool(accumulate)),
+                                      _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                      s), "halp_mx4_product")
+
+
+def mx4_row_product(x, w, out, stream=None):
+    """out [M, N] = x [M, K], quantized to the nearest on the way, times w [N, K]^T; M <= 16."""
+    ldx, ldy = _matrix(x, "x", (x.shape[0], w.cols)), _matrix(out, "out", (x.shape[0], w.rows))
+    dev, s = _on(stream, x, w.codes, out)
+    with dev:
+        _check(lib().halp_mx4_row_product(_ptr(x), _type(x, "x"), x.shape[0], ldx, C.byref(w.c), _ptr(out),
+                                          _type(out, "out"), ldy, s), "halp_mx4_row_product")
+
+
+class AdamW:
+    """The AdamW step of a list of tensors as one launch.  tensors: dicts of contiguous GPU tensors
+    p (float32), g (one of three types, the same for all), m, v (float32; with state_bits 8 uint8 codes), with
+    state_bits 8 also m_scale, v_scale (uint8, ceil(n / 32)), and optionally copy (the new p in a
+    narrower type).  The handle keeps references to them."""
+
+    def __init__(self, tensors, state_bits=32, seed=0):
+        self._h = C.c_void_p()
+        tensors = [dict(t) for t in tensors]
+        if not tensors:
+            raise ValueError("at least one tensor expected")
+        self._keep = tensors
+        state, dev = ("torch.float32" if state_bits == 32 else "torch.uint8"), tensors[0]["p"].device
+        copies = {_type(t["copy"], "copy") for t in tensors if t.get("copy") is not None}
+        grads = {_type(t["g"], "g") for t in tensors}
+        if len(grads) > 1 or len(copies) > 1:
+            raise ValueError("all g have one type, and all copy")
+        arr = (AdamWTensor * len(tensors))()
+        for a, t in zip(arr, tensors):
+            a.n = t["p"].numel()
+            want = {"p": "torch.float32", "g": None, "copy": None, "m": state, "v": state}
+            if state_bits == 8:
+                want |= {"m_scale": "torch.uint8", "v_scale": "torch.uint8"}
+            for name, dtype in want.items():
+                x = t.get(name)
+                if x is None:
+                    if name != "copy":
+                        raise ValueError(f"{name} is missing")
+                    continue
+                if (dtype is not None and str(x.dtype) != dtype) or not x.is_contiguous() or x.device != dev:
+                    raise ValueError(f"{name}: a contiguous {dtype or 'floating-point'} tensor on {dev} expected")
+                if x.numel() != ((a.n + 31) // 32 if name.endswith("_scale") else a.n):
+                    raise ValueError(f"{name}: {x.numel()} elements for a tensor of {a.n}")
+                setattr(a, name, x.data_ptr())
+        with _on(None, tensors[0]["p"])[0]:
+            _check(lib().halp_adamw_create(C.byref(self._h), arr, len(tensors), state_bits, grads.pop(),
+                                           copies.pop() if copies else TYPE_BF16, seed & (2 ** 64 - 1)), "halp_adamw_create")
+
+    def close(self):
+        if self._h:
+            lib().halp_adamw_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, step=1, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=None, step_at=None,
+             lr_at=None, stream=None):
+        """One step.  step counts from 1; step_at (int64) and lr_at (float32), one-element GPU tensors, take the place of
+        step and lr where given; grad_scale (float32, one element) scales the gradients and skips the step where it
+        is not finite."""
+        for name, t, dtype in (("grad_scale", grad_scale, "torch.float32"), ("step_at", step_at, "torch.int64"),
+                               ("lr_at", lr_at, "torch.float32")):
+            if t is not None and (str(t.dtype) != dtype or t.numel() != 1):
+                raise ValueError(f"{name}: one {dtype} expected")
+        a = AdamWArgs(lr, beta1, beta2, eps, weight_decay, step, _ptr(step_at), _ptr(lr_at), _ptr(grad_scale))
+        dev, s = _on(stream, self._keep[0]["p"], grad_scale, step_at, lr_at)
+        with dev:
+            _check(lib().halp_adamw_step(self._h, C.byref(a), s), "halp_adamw_step")
+
+    def grad_norm(self, max_norm, out, stream=None):
+        """out (float32 [2]): the norm of all gradients, and the grad_scale that clips it to max_norm."""
+        if str(out.dtype) != "torch.float32" or out.numel() != 2 or not out.is_contiguous():
+            raise ValueError("out: two contiguous float32 expected")
+        dev, s = _on(stream, self._keep[0]["p"], out)
+        with dev:
+            _check(lib().halp_adamw_grad_norm(self._h, max_norm, _ptr(out), s), "halp_adamw_grad_norm")
+
+
+def adamw_read_moments(m, m_scale, v, v_scale, m_out, v_out, stream=None):
+    """The values of 8-bit states (uint8 codes and scales) as float32."""
+    n = m.numel()
+    for name, t, dtype, k in (("m", m, "torch.uint8", n), ("m_scale", m_scale, "torch.uint8", (n + 31) // 32),
+                              ("v", v, "torch.uint8", n), ("v_scale", v_scale, "torch.uint8", (n + 31) // 32),
+                              ("m_out", m_out, "torch.float32", n), ("v_out", v_out, "torch.float32", n)):
+        if str(t.dtype) != dtype or t.numel() != k or not t.is_contiguous():
+            raise ValueError(f"{name}: {k} contiguous {dtype} expected")
+    dev, s = _on(stream, m, m_scale, v, v_scale, m_out, v_out)
+    with dev:
+        _check(lib().halp_adamw_read_moments(_ptr(m), _ptr(m_scale), _ptr(v), _ptr(v_scale), n, _ptr(m_out), _ptr(v_out), s),
+               "halp_adamw_read_moments")

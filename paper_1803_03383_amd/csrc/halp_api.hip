@@ -17,13 +17,6 @@ namespace {
 // text of the last failed HIP runtime call on this thread, for halp_last_error_detail
 thread_local char g_detail[256] = "";
 
-bool hip_fail(hipError_t e, const char* what) {
-  if (e == hipSuccess) return false;
-  std::snprintf(g_detail, sizeof g_detail, "%s: %s", what, hipGetErrorString(e));
-  (void)hipGetLastError();
-  return true;
-}
-
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 int check_params(const halp_params& p) {
@@ -180,6 +173,13 @@ int need_inner(const halp_handle& h, int variant) {
 }
 
 }  // namespace
+
+bool halp::hip_fail(hipError_t e, const char* what) {
+  if (e == hipSuccess) return false;
+  std::snprintf(g_detail, sizeof g_detail, "%s: %s", what, hipGetErrorString(e));
+  (void)hipGetLastError();
+  return true;
+}
 
 extern "C" {
 

@@ -10,7 +10,9 @@ namespace halp {
 
 constexpr int kWave = 64;
 
-enum Purpose : uint32_t { kIdx = 0, kGamma = 1, kZround = 2, kReg = 3, kHround = 4, kOpt2 = 5 };
+enum Purpose : uint32_t {
+  kIdx = 0, kGamma = 1, kZround = 2, kReg = 3, kHround = 4, kOpt2 = 5, kMx4Rows = 6, kMx4Cols = 7, kMoments = 8
+};
 
 struct U4 {
   uint32_t x, y, z, w;

@@ -125,6 +125,8 @@ int launch_debug_step_latency(int waves, int64_t steps, int blocks, uint32_t* ou
 int launch_debug_zround_bits(uint64_t seed, uint32_t epoch, uint64_t t, int32_t d, int32_t b,
                              int32_t K, uint32_t* out, hipStream_t s);
 
+// true where e is an error; keeps its text for halp_last_error_detail
+bool hip_fail(hipError_t e, const char* what);
 inline int hip_ok(hipError_t e) { return e == hipSuccess ? HALP_OK : HALP_ERR_HIP; }
 
 }  // namespace halp

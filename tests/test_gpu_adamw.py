@@ -1,0 +1,315 @@
+"""The AdamW step over many tensors on the GPU against the oracle: 32-bit states within the roundings of
+the formula, 8-bit states code for code, p within its roundings in both."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1803_03383_amd as hp
+from oracle import adamw
+
+pytestmark = pytest.mark.gpu
+
+H = 2.0 ** -24  # half a step of fp32, relative
+GRADS = [torch.float32, torch.bfloat16, torch.float16]
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.02)
+SIZES = [1, 2, 31, 32, 33, 127, 4095, 4096, 4097, 10001, 3, 0, 70000]
+
+
+def _tensors(sizes, bits, grad, copy=None, seed=0, offset=0, fresh=False):
+    """Tensors at `offset` elements into buffers of their own, with a guard behind."""
+    r = np.random.default_rng(seed)
+    out = []
+    for n in sizes:
+        def put(v, dtype):
+            buf = torch.full((offset + n + 7,), 77, dtype=dtype, device="cuda")
+            buf[offset:offset + n] = torch.from_numpy(np.asarray(v)).to(dtype)
+            return buf[offset:offset + n]
+        g = r.standard_normal(n) * np.exp(r.standard_normal(n)) * 1e-2
+        t = dict(p=put(r.standard_normal(n), torch.float32), g=put(g, grad))
+        m, v = r.standard_normal(n) * 1e-2, np.exp(2 * r.standard_normal(n)) * 1e-4
+        if fresh:
+            m, v = m * 0, v * 0
+        if bits == 32:
+            t |= dict(m=put(m, torch.float32), v=put(v, torch.float32))
+        else:
+            for k, x in (("m", m), ("v", v)):
+                codes, scales = adamw.write(x.astype(np.float32), np.full(n, 0x8000), k)
+                t[k] = put(codes, torch.uint8)
+                t[k + "_scale"] = put(scales, torch.uint8) if len(scales) == n else torch.from_numpy(scales).cuda()
+        if copy is not None:
+            t["copy"] = put(np.zeros(n), copy)
+        out.append(t)
+    return out
+
+
+def _host(t):
+    return {k: (v.float() if v.dtype in (torch.bfloat16, torch.float16) else v).cpu().numpy().copy() for k, v in t.items()}
+
+
+def _check(before, t, i, step, bits, seed, scale=1.0, hyper=HYPER):
+    lr, b1, b2, eps, decay = (hyper[k] for k in ("lr", "beta1", "beta2", "eps", "weight_decay"))
+    old, new = before[i], _host(t)
+    n = len(old["p"])
+    g = old["g"].astype(np.float64) * scale
+    if bits == 32:
+        m0, v0 = old["m"].astype(np.float64), old["v"].astype(np.float64)
+    else:
+        m0, v0 = adamw.read(old["m"], old["m_scale"], "m"), adamw.read(old["v"], old["v_scale"], "v")
+    p, m, v = adamw.step(old["p"].astype(np.float64), old["g"], m0, v0, step, lr, b1, b2, eps, decay, scale)
+    # m: beta1, its product and the sum; g', 1 - beta1, their product and the sum.  v likewise, with g' twice and its square
+    dm = H * (3 * np.abs(b1 * m0) + 4 * np.abs((1 - b1) * g)) * 1.01 + 2.0 ** -148
+    dv = H * (3 * b2 * v0 + 6 * (1 - b2) * g * g) * 1.01 + 2.0 ** -148
+    if bits == 32:
+        assert (np.abs(new["m"] - m) <= dm).all() and (np.abs(new["v"] - v) <= dv).all()
+    else:
+        m32, v32 = adamw.moments32(old["g"], m0.astype(np.float32), v0.astype(np.float32), b1, b2, scale)
+        words = adamw.random_words(n, step, seed + i)
+        for k, x, w in (("m", m32, words & 0xFFFF), ("v", v32, words >> 16)):
+            codes, scales = adamw.write(x, w, k)
+            assert np.array_equal(new[k + "_scale"], scales)
+            assert np.array_equal(new[k], codes)
+    # the update's errors: of m over the denominator, half of v's relative one, and eight roundings of its own
+    # (root, its factor and product, eps' sum, quotient, rate, product); p's: its factor, product and the difference
+    rate, den = lr / (1 - b1 ** step), np.sqrt(v / (1 - b2 ** step)) + eps
+    upd = rate * np.abs(m) / den
+    rel_v = np.where(v > 0, dv / np.where(v > 0, v, 1), 0)
+    dp = rate * dm / den + upd * (8 * H + rel_v) + H * (2 * np.abs(old["p"]) + np.abs(p)) * 1.01
+    assert (np.abs(new["p"] - p) <= dp).all()
+    if "copy" in t:
+        assert torch.equal(t["copy"].cpu(), t["p"].cpu().to(t["copy"].dtype))
+
+
+@pytest.mark.parametrize("offset", [0, 1, 4])
+@pytest.mark.parametrize("grad", GRADS, ids=str)
+@pytest.mark.parametrize("bits", [8, 32])
+def test_steps_of_many_tensors(bits, grad, offset):
+    tensors = _tensors(SIZES, bits, grad, offset=offset)
+    plan = hp.AdamW(tensors, state_bits=bits, seed=2 ** 63 + 5)
+    for step in (1, 2, 1000, 2 ** 32 - 1):
+        before = [_host(t) for t in tensors]
+        plan.step(step, **HYPER)
+        torch.cuda.synchronize()
+        for i, t in enumerate(tensors):
+            _check(before, t, i, step, bits, 2 ** 63 + 5)
+            for x in t.values():  # what lies around a tensor stays
+                base = x._base if x._base is not None else x
+                if base.numel() == x.numel() + offset + 7:
+                    assert (base[:offset] == 77).all() and (base[offset + x.numel():] == 77).all()
+
+
+@pytest.mark.parametrize("copy", GRADS, ids=str)
+@pytest.mark.parametrize("bits", [8, 32])
+def test_first_steps_with_a_copy_and_a_gradient_scale(bits, copy):
+    tensors = _tensors([5000, 129], bits, torch.float32, copy=copy, fresh=True)
+    plan = hp.AdamW(tensors, state_bits=bits, seed=1)
+    scale = torch.tensor([0.37], device="cuda")
+    for step in (1, 2, 3):
+        before = [_host(t) for t in tensors]
+        plan.step(step, grad_scale=scale, **HYPER)
+        for i, t in enumerate(tensors):
+            _check(before, t, i, step, bits, 1, scale=float(scale))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_hyperparameters_at_their_edges(bits):
+    for hyper in (dict(HYPER, beta1=0.0), dict(HYPER, beta2=0.0), dict(HYPER, weight_decay=0.0), dict(HYPER, lr=0.0), dict(HYPER, eps=1.0)):
+        tensors = _tensors([300], bits, torch.float32)
+        before = [_host(t) for t in tensors]
+        hp.AdamW(tensors, state_bits=bits).step(7, **hyper)
+        _check(before, tensors[0], 0, 7, bits, 0, hyper=hyper)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_scale_that_is_not_finite_skips_the_step(bits):
+    tensors = _tensors([100, 5000], bits, torch.bfloat16)
+    before = [_host(t) for t in tensors]
+    plan = hp.AdamW(tensors, state_bits=bits)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        plan.step(1, grad_scale=torch.tensor([bad], device="cuda"))
+    for bad in (0, -1, 2 ** 32):
+        plan.step(step_at=torch.tensor([bad], device="cuda"))
+    for b, t in zip(before, tensors):
+        assert all(np.array_equal(b[k], v) for k, v in _host(t).items())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_gradients_that_are_not_finite(bits):
+    """Spoil their element, with 8-bit states their block, and nothing else."""
+    tensors = _tensors([200], bits, torch.float32)
+    t = tensors[0]
+    t["g"][70], t["g"][130] = float("nan"), float("inf")
+    hp.AdamW(tensors, state_bits=bits).step(5, **HYPER)
+    p = t["p"].cpu().numpy()
+    assert np.isnan(p[[70, 130]]).all() and np.isfinite(np.delete(p, [70, 130])).all()
+    if bits == 8:
+        assert t["m_scale"].cpu().tolist()[2] == 255 and t["v_scale"].cpu().tolist()[4] == 255
+        assert all(s < 255 for i, s in enumerate(t["m_scale"].cpu().tolist()) if i not in (2, 4))
+        m, v = torch.empty(200, device="cuda"), torch.empty(200, device="cuda")
+        hp.adamw_read_moments(t["m"], t["m_scale"], t["v"], t["v_scale"], m, v)
+        assert torch.isnan(m[64:96]).all() and torch.isnan(v[128:160]).all() and torch.isfinite(m[:64]).all()
+
+
+def test_tiny_and_huge_gradients_in_8_bits():
+    """Moments from subnormal to near the largest number: scales at both ends."""
+    r = np.random.default_rng(4)
+    tensors = _tensors([320], 8, torch.float32, fresh=True)
+    mags = np.repeat(10.0 ** np.linspace(-22, 18, 10), 32)
+    tensors[0]["g"].copy_(torch.from_numpy(r.standard_normal(320) * mags))
+    plan = hp.AdamW(tensors, state_bits=8, seed=3)
+    for step in (1, 2, 3):
+        before = [_host(t) for t in tensors]
+        plan.step(step, **HYPER)
+        _check(before, tensors[0], 0, step, 8, 3)
+
+
+def test_reading_every_state():
+    codes = np.tile(np.arange(256, dtype=np.uint8), 256)
+    for k, other in (("m", "v"), ("v", "m")):
+        scales = np.repeat(np.arange(256, dtype=np.uint8), 8)
+        m_out, v_out = torch.empty(65536, device="cuda"), torch.empty(65536, device="cuda")
+        c, s = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+        hp.adamw_read_moments(c, s, c, s, m_out, v_out)
+        got = (m_out if k == "m" else v_out).double().cpu().numpy()
+        with np.errstate(over="ignore"):
+            want = adamw.read(codes, scales, k).astype(np.float32).astype(np.float64)
+        used = (codes & 127) < 127 if k == "m" else codes < 248  # the others are never written
+        assert np.array_equal(got[used], want[used], equal_nan=True)
+
+
+@pytest.mark.parametrize("grad", GRADS, ids=str)
+@pytest.mark.parametrize("sizes", [[1], [5, 0, 4096, 4097, 3], [300_000, 77] * 9])
+def test_norm_and_clipping(sizes, grad):
+    tensors = _tensors(sizes, 32, grad, offset=1)
+    plan = hp.AdamW(tensors)
+    out = torch.empty(2, device="cuda")
+    want = np.sqrt(sum(float((t["g"].double() ** 2).sum()) for t in tensors))
+    for most in (want / 3, want * 3):
+        plan.grad_norm(most, out)
+        assert abs(float(out[0]) - want) <= 2 * H * want
+        assert abs(float(out[1]) - min(1.0, most / want)) <= 2 * H
+    before = [_host(t) for t in tensors]
+    plan.grad_norm(want / 3, out)
+    plan.step(4, grad_scale=out[1:], **HYPER)
+    for i, t in enumerate(tensors):
+        _check(before, t, i, 4, 32, 0, scale=float(out[1]))
+
+
+def test_norms_at_the_ends():
+    tensors = _tensors([5000, 40], 32, torch.float32)
+    plan, out = hp.AdamW(tensors), torch.empty(2, device="cuda")
+    tensors[0]["g"].zero_()
+    tensors[1]["g"].zero_()
+    plan.grad_norm(1.0, out)
+    assert out.tolist() == [0.0, 1.0]
+    tensors[1]["g"].fill_(1e30)  # squares past fp32
+    plan.grad_norm(1.0, out)
+    want = float(np.float32(1e30)) * 40 ** 0.5
+    assert abs(float(out[0]) / want - 1) <= 2 * H and abs(float(out[1]) * want - 1) <= 2 * H
+    for bad in (float("inf"), float("nan")):
+        tensors[0]["g"][4999] = bad
+        plan.grad_norm(1.0, out)
+        assert not np.isfinite(float(out[0])) and np.isnan(float(out[1]))
+        before = [_host(t) for t in tensors]
+        plan.step(1, grad_scale=out[1:])
+        assert all(np.array_equal(b[k], v) for b, t in zip(before, tensors) for k, v in _host(t).items() if k != "g")
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(lr=-1.0), hp.ERR_INVALID), (dict(lr=float("nan")), hp.ERR_INVALID), (dict(beta1=1.0), hp.ERR_INVALID),
+    (dict(beta2=-0.1), hp.ERR_INVALID), (dict(eps=0.0), hp.ERR_INVALID), (dict(eps=1e-50), hp.ERR_INVALID),
+    (dict(weight_decay=float("inf")), hp.ERR_INVALID), (dict(step=0), hp.ERR_INVALID), (dict(step=2 ** 32), hp.ERR_INVALID)])
+def test_refused_steps(kw, code):
+    tensors = _tensors([10], 32, torch.float32)
+    before = _host(tensors[0])
+    plan = hp.AdamW(tensors)
+    with pytest.raises(hp.HalpError) as e:
+        plan.step(**dict(dict(step=1), **kw))
+    assert e.value.code == code
+    with pytest.raises(hp.HalpError):
+        plan.grad_norm(0.0, torch.empty(2, device="cuda"))
+    for bad in (dict(grad_scale=torch.zeros(2, device="cuda")), dict(step_at=torch.zeros(1, device="cuda")), dict(lr_at=torch.zeros(1))):
+        with pytest.raises(ValueError):
+            plan.step(1, **bad)
+    assert all(np.array_equal(before[k], v) for k, v in _host(tensors[0]).items())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_captured_step_counts_and_follows_the_learning_rate(bits):
+    """Replays with new gradients, the step and the rate in device memory, against eager steps of the same numbers."""
+    a, b = (_tensors([3000, 50, 7], bits, torch.bfloat16, copy=torch.bfloat16, seed=5) for _ in range(2))
+    pa, pb = hp.AdamW(a, state_bits=bits, seed=8), hp.AdamW(b, state_bits=bits, seed=8)
+    t, lr, norm = torch.ones(1, dtype=torch.int64, device="cuda"), torch.full((1,), 1e-3, device="cuda"), torch.empty(2, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pa.grad_norm(0.5, norm)
+        pa.step(step_at=t, lr_at=lr, grad_scale=norm[1:])
+        t.add_(1)
+    want = torch.empty(2, device="cuda")
+    for step in range(1, 6):
+        rate = np.float32(1e-3 / step)
+        lr.fill_(float(rate))
+        for x, y in zip(a, b):
+            g = torch.randn(x["g"].numel(), device="cuda").bfloat16()
+            x["g"].copy_(g)
+            y["g"].copy_(g)
+        graph.replay()
+        pb.grad_norm(0.5, want)
+        pb.step(step, lr=float(rate), grad_scale=want[1:])
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want) and int(t) == step + 1
+        for x, y in zip(a, b):
+            assert all(torch.equal(x[k], y[k]) for k in x), step
+
+
+def test_another_stream_and_the_same_bits_again():
+    outs = []
+    for stream in (None, torch.cuda.Stream()):
+        tensors = _tensors([9000, 123], 8, torch.float16, seed=6)
+        plan = hp.AdamW(tensors, state_bits=8, seed=1)
+        torch.cuda.synchronize()
+        for step in (1, 2):
+            plan.step(step, stream=None if stream is None else stream.cuda_stream)
+        torch.cuda.synchronize()
+        outs.append([t[k] for t in tensors for k in ("p", "m", "v", "m_scale", "v_scale")])
+    assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_layer_is_trained(bits):
+    """Two steps of a linear layer with 4-bit operands: forward, both gradients and the update, against the
+    formulas in 64 bits on the values the operators were given."""
+    from oracle import mx4
+    r = np.random.default_rng(7)
+    M, N, K = 150, 70, 200
+    x, w0, target = r.standard_normal((M, K)), r.standard_normal((N, K)) / K ** 0.5, r.standard_normal((M, N))
+    xg = torch.from_numpy(x).cuda().bfloat16()
+    tensors = _tensors([N * K], bits, torch.float32, fresh=True)
+    tensors[0]["p"].copy_(torch.from_numpy(w0.reshape(-1)))
+    w, dw = tensors[0]["p"].view(N, K), tensors[0]["g"].view(N, K)
+    plan = hp.AdamW(tensors, state_bits=bits, seed=2)
+    f = {k: hp.mx4_empty(*s) for k, s in dict(xq=(M, K), xt=(K, M), wq=(N, K), wt=(K, N), dq=(M, N), dt=(N, M)).items()}
+    y, dx = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda")
+
+    def val(a):  # the values of both forms, from the oracle
+        a = a.double().cpu().numpy()
+        return mx4.values(*mx4.quantize(a))[:, :a.shape[1]], mx4.values(*mx4.quantize(a.T))[:, :a.shape[0]]
+
+    def close(got, a, b):
+        want = a.dot(b.T)
+        assert (np.abs(got.double().cpu().numpy() - want) <= (a.shape[1] + 1) * 2.0 ** -23 * np.abs(a).dot(np.abs(b).T)).all()
+
+    for step in (1, 2):
+        hp.mx4_quantize(xg, f["xq"], f["xt"])
+        hp.mx4_quantize(w, f["wq"], f["wt"])
+        hp.mx4_product(f["xq"], f["wq"], y)
+        dy = (y - torch.from_numpy(target).cuda().float()) / M
+        hp.mx4_quantize(dy, f["dq"], f["dt"])
+        hp.mx4_product(f["dq"], f["wt"], dx)
+        hp.mx4_product(f["dt"], f["xt"], dw)
+        (xv, xtv), (wv, wtv), (dv, dtv) = val(xg), val(w), val(dy)
+        close(y, xv, wv)
+        close(dx, dv, wtv)
+        close(dw, dtv, xtv)
+        before = [_host(t) for t in tensors]
+        plan.step(step, **HYPER)
+        _check(before, tensors[0], 0, step, bits, 2)

@@ -1,0 +1,138 @@
+"""What the 4-bit microscaled operators and AdamW refuse, through the C ABI and without a GPU: every
+check answers before anything touches a device (the pointers here are never dereferenced)."""
+import ctypes as C
+
+import pytest
+
+import paper_1803_03383_amd as hp
+
+FAKE = 1 << 20
+
+
+def _mx(rows=8, cols=200, **kw):
+    q = hp.Mx4Struct(FAKE, 128, FAKE, 8, rows, cols)
+    for k, v in kw.items():
+        setattr(q, k, v)
+    return q
+
+
+BAD_MATRIX = [(dict(rows=-1), hp.ERR_INVALID), (dict(rows=2 ** 31), hp.ERR_INVALID), (dict(codes=None), hp.ERR_NULL),
+              (dict(scales=None), hp.ERR_NULL), (dict(ldc=112), hp.ERR_INVALID), (dict(ldc=136), hp.ERR_ALIGN),
+              (dict(lds=4), hp.ERR_INVALID), (dict(lds=10), hp.ERR_ALIGN), (dict(codes=FAKE + 8), hp.ERR_ALIGN),
+              (dict(scales=FAKE + 2), hp.ERR_ALIGN), (dict(ldc=2 ** 40), hp.ERR_INVALID)]
+
+
+@pytest.mark.parametrize("kw,code", BAD_MATRIX)
+def test_a_matrix_that_does_not_hold_its_rows(kw, code):
+    L, bad, ok = hp.lib(), _mx(**kw), _mx()
+    rows = max(bad.rows, 0) if bad.rows < 2 ** 31 else 8
+    assert L.halp_mx4_dequantize(C.byref(bad), FAKE, 0, 200, None) == code
+    assert L.halp_mx4_product(C.byref(bad), C.byref(ok), FAKE, 0, 8, 0, None, 0, None) == code
+    assert L.halp_mx4_product(C.byref(ok), C.byref(bad), FAKE, 0, 8, 0, None, 0, None) == code
+    assert L.halp_mx4_row_product(FAKE, 0, 4, 200, C.byref(bad), FAKE, 0, 8, None) == code
+    if "rows" not in kw:
+        assert L.halp_mx4_quantize(FAKE, 0, rows, 200, 200, C.byref(bad), None, 0, 0, 0, None) == code
+        turned = _mx(rows=200, **kw)
+        assert L.halp_mx4_quantize(FAKE, 0, 200, 200, 200, None, C.byref(turned), 0, 0, 0, None) == code
+
+
+def _quantize(q=None, qt=None, x=FAKE, type=0, rows=8, cols=200, ldx=200, rounding=0, epoch=0):
+    return hp.lib().halp_mx4_quantize(x, type, rows, cols, ldx, q, qt, rounding, 0, epoch, None)
+
+
+def test_quantize():
+    q = C.byref(_mx())
+    assert _quantize() == hp.ERR_NULL
+    assert _quantize(q, x=None) == hp.ERR_NULL
+    for kw in (dict(type=3), dict(type=-1), dict(rows=9), dict(cols=199), dict(ldx=199), dict(rounding=2), dict(epoch=-1),
+               dict(epoch=2 ** 32), dict(rows=-1)):
+        assert _quantize(q, **kw) == hp.ERR_INVALID, kw
+    assert _quantize(q, x=FAKE + 2) == hp.ERR_ALIGN
+    assert _quantize(q, x=FAKE + 1, type=1) == hp.ERR_ALIGN
+    assert _quantize(None, C.byref(_mx())) == hp.ERR_INVALID  # not the transpose's shape
+    assert _quantize(C.byref(_mx(rows=0)), rows=0) == 0  # nothing to write
+
+
+def test_product():
+    L = hp.lib()
+
+    def product(a=None, b=None, c=FAKE, type=0, ldc=8, add=0, ws=None, n=0):
+        return L.halp_mx4_product(C.byref(a or _mx()), C.byref(b or _mx()), c, type, ldc, add, ws, n, None)
+
+    assert L.halp_mx4_product(None, C.byref(_mx()), FAKE, 0, 8, 0, None, 0, None) == hp.ERR_NULL
+    assert product(c=None) == hp.ERR_NULL
+    for kw in (dict(b=_mx(cols=199)), dict(type=5), dict(ldc=7), dict(add=2), dict(n=-1)):
+        assert product(**kw) == hp.ERR_INVALID, kw
+    assert product(type=hp.TYPE_BF16, add=1) == hp.ERR_UNSUPPORTED
+    assert product(c=FAKE + 2) == hp.ERR_ALIGN
+    assert product(ws=FAKE + 8, n=1 << 20) == hp.ERR_ALIGN
+    assert product(a=_mx(rows=0)) == 0 and product(b=_mx(rows=0)) == 0  # nothing to write
+    assert L.halp_mx4_product_workspace(1, 1, 1, None) == hp.ERR_NULL
+    n = C.c_int64()
+    assert L.halp_mx4_product_workspace(-1, 1, 1, C.byref(n)) == hp.ERR_INVALID
+
+
+def test_row_product():
+    L = hp.lib()
+
+    def product(x=FAKE, xt=0, M=4, ldx=200, y=FAKE, yt=0, ldy=8):
+        return L.halp_mx4_row_product(x, xt, M, ldx, C.byref(_mx()), y, yt, ldy, None)
+
+    assert product(M=17) == hp.ERR_UNSUPPORTED
+    assert product(x=None) == hp.ERR_NULL and product(y=None) == hp.ERR_NULL
+    for kw in (dict(M=-1), dict(xt=3), dict(yt=-1), dict(ldx=199), dict(ldy=7)):
+        assert product(**kw) == hp.ERR_INVALID, kw
+    assert product(x=FAKE + 1, xt=1) == hp.ERR_ALIGN and product(y=FAKE + 2) == hp.ERR_ALIGN
+    assert product(M=0) == 0
+
+
+def _tensor(**kw):
+    t = hp.AdamWTensor(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, 100)
+    for k, v in kw.items():
+        setattr(t, k, v)
+    return t
+
+
+@pytest.mark.parametrize("kw,bits,code", [
+    (dict(n=-1), 32, hp.ERR_INVALID), (dict(n=2 ** 40), 32, hp.ERR_INVALID), (dict(p=None), 32, hp.ERR_NULL),
+    (dict(g=None), 32, hp.ERR_NULL), (dict(m=None), 32, hp.ERR_NULL), (dict(v=None), 8, hp.ERR_NULL),
+    (dict(m_scale=None), 8, hp.ERR_NULL), (dict(v_scale=None), 8, hp.ERR_NULL), (dict(p=FAKE + 2), 32, hp.ERR_ALIGN),
+    (dict(g=FAKE + 2), 32, hp.ERR_ALIGN), (dict(v=FAKE + 1), 32, hp.ERR_ALIGN), (dict(copy=FAKE + 1), 32, hp.ERR_ALIGN),
+    (dict(), 16, hp.ERR_UNSUPPORTED),
+])
+def test_adamw_create(kw, bits, code):
+    h = C.c_void_p()
+    assert hp.lib().halp_adamw_create(C.byref(h), C.byref(_tensor(**kw)), 1, bits, hp.TYPE_F32, hp.TYPE_BF16, 0) == code
+    assert not h.value
+
+
+def test_adamw_calls():
+    L, h, t = hp.lib(), C.c_void_p(), _tensor()
+    assert L.halp_adamw_create(None, C.byref(t), 1, 32, 0, 0, 0) == hp.ERR_NULL
+    assert L.halp_adamw_create(C.byref(h), None, 1, 32, 0, 0, 0) == hp.ERR_NULL
+    for count, gt, ct in ((0, 0, 0), (2 ** 24, 0, 0), (1, 3, 0), (1, 0, -1)):
+        assert L.halp_adamw_create(C.byref(h), C.byref(t), count, 32, gt, ct, 0) == hp.ERR_INVALID
+    assert L.halp_adamw_destroy(None) == hp.ERR_NULL
+    assert L.halp_adamw_step(None, C.byref(hp.AdamWArgs()), None) == hp.ERR_NULL
+    assert L.halp_adamw_grad_norm(None, 1.0, FAKE, None) == hp.ERR_NULL
+    read = L.halp_adamw_read_moments
+    assert read(FAKE, FAKE, FAKE, FAKE, -1, FAKE, FAKE, None) == hp.ERR_INVALID
+    assert read(FAKE, None, FAKE, FAKE, 1, FAKE, FAKE, None) == hp.ERR_NULL
+    assert read(FAKE, FAKE, FAKE, FAKE, 1, FAKE + 2, FAKE, None) == hp.ERR_ALIGN
+    assert read(None, None, None, None, 0, None, None, None) == 0
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    import torch
+    x = torch.zeros(4, 200)
+    q = hp.mx4_empty(4, 200, device="cpu")
+    for bad in (lambda: hp.mx4_quantize(x, q), lambda: hp.mx4_quantize(x.t(), q), lambda: hp.mx4_quantize(x[0], q),
+                lambda: hp.mx4_dequantize(q, x[:, :100]), lambda: hp.mx4_product(q, q, x), lambda: hp.mx4_row_product(x[:, :64], q, x),
+                lambda: hp.Mx4(q.codes, q.scales, 300), lambda: hp.Mx4(q.codes[:2], q.scales, 200), lambda: hp.Mx4(x, q.scales, 200),
+                lambda: hp.AdamW([]), lambda: hp.AdamW([dict(p=x, g=x, m=x)]), lambda: hp.AdamW([dict(p=x, g=x, m=x, v=x[:2])]),
+                lambda: hp.AdamW([dict(p=x, g=x, m=x, v=x)], state_bits=8),
+                lambda: hp.AdamW([dict(p=x, g=x, m=x, v=x, copy=x.int())]),
+                lambda: hp.AdamW([dict(p=x, g=x, m=x, v=x), dict(p=x, g=x.half(), m=x, v=x)]),
+                lambda: hp.adamw_read_moments(q.codes, q.scales, q.codes, q.scales, x, x)):
+        with pytest.raises(ValueError):
+            bad()
