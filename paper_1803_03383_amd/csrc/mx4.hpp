@@ -13,6 +13,8 @@ namespace halp {
 using v2bf16 = __bf16 __attribute__((ext_vector_type(2)));
 using v2f16 = _Float16 __attribute__((ext_vector_type(2)));
 using v4f32 = float __attribute__((ext_vector_type(4)));
+using v16f32 = float __attribute__((ext_vector_type(16)));
+using v4i32 = int __attribute__((ext_vector_type(4)));
 using v8i32 = int __attribute__((ext_vector_type(8)));
 
 constexpr int kMxBlock = 32;   // values per scale
@@ -89,7 +91,7 @@ int launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols,
                         const MxView* qt, int32_t rounding, uint64_t seed, uint32_t epoch, hipStream_t s);
 int launch_mx4_dequantize(const MxView& q, void* out, int32_t type, int64_t ldo, hipStream_t s);
 int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, int64_t ldc, bool accumulate,
-                       void* workspace, int64_t workspace_bytes, hipStream_t s);
+                       void* workspace, int64_t workspace_bytes, int cus, hipStream_t s);
 int64_t mx4_product_workspace(int64_t M, int64_t N, int64_t K, int cus);
 int launch_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, const MxView& w, void* y,
                            int32_t ytype, int64_t ldy, hipStream_t s);

@@ -10,11 +10,11 @@ bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % 
 constexpr int64_t kMost = int64_t(1) << 31;
 
 int check_matrix(const halp_mx4& q) {
-  if (q.rows < 0 || q.cols < 0 || q.rows >= kMost || q.cols >= kMost) return HALP_ERR_INVALID;
+  if (q.rows < 0 || q.cols < 0 || q.rows >= kMost || q.cols >= (int64_t(1) << 24)) return HALP_ERR_INVALID;
   if (q.rows == 0 || q.cols == 0) return HALP_OK;  // nothing is stored
   if (!q.codes || !q.scales) return HALP_ERR_NULL;
   if (q.ldc < 64 * mx_groups(q.cols) || q.lds < 4 * mx_groups(q.cols)) return HALP_ERR_INVALID;
-  if (q.ldc >= (int64_t(1) << 40) || q.lds >= (int64_t(1) << 40)) return HALP_ERR_INVALID;
+  if (q.ldc >= (1 << 23) || q.lds >= (1 << 23)) return HALP_ERR_INVALID;  // a tile's rows are within 32 bits
   if (q.ldc % 16 || q.lds % 4 || !aligned(q.codes, 16) || !aligned(q.scales, 4)) return HALP_ERR_ALIGN;
   return HALP_OK;
 }
@@ -26,6 +26,15 @@ int check_plain(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t
   if (!x) return HALP_ERR_NULL;
   if (ld < cols || ld >= (int64_t(1) << 40)) return HALP_ERR_INVALID;
   return aligned(x, type_bytes(type)) ? HALP_OK : HALP_ERR_ALIGN;
+}
+
+// compute units of the current device
+int count_cus(int* cus) {
+  int dev = 0;
+  if (hip_fail(hipGetDevice(&dev), "hipGetDevice") ||
+      hip_fail(hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev), "hipDeviceGetAttribute"))
+    return HALP_ERR_HIP;
+  return HALP_OK;
 }
 
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
@@ -72,17 +81,17 @@ int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type
   if (accumulate && type != HALP_TYPE_F32) return HALP_ERR_UNSUPPORTED;
   if (workspace && !aligned(workspace, 16)) return HALP_ERR_ALIGN;
   if (a->rows == 0 || b->rows == 0) return HALP_OK;
+  int cus = 0;
+  if ((rc = count_cus(&cus)) != HALP_OK) return rc;
   return launch_mx4_product(mx_view(*a), mx_view(*b), c, type, ldc, accumulate != 0, workspace,
-                            workspace ? workspace_bytes : 0, as_stream(stream));
+                            workspace ? workspace_bytes : 0, cus, as_stream(stream));
 }
 
 int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes) {
   if (!bytes) return HALP_ERR_NULL;
   if (M < 0 || N < 0 || K < 0 || M >= kMost || N >= kMost || K >= kMost) return HALP_ERR_INVALID;
-  int dev = 0, cus = 0;
-  if (hip_fail(hipGetDevice(&dev), "hipGetDevice") ||
-      hip_fail(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev), "hipDeviceGetAttribute"))
-    return HALP_ERR_HIP;
+  int cus = 0;
+  if (const int rc = count_cus(&cus)) return rc;
   *bytes = mx4_product_workspace(M, N, K, cus);
   return HALP_OK;
 }

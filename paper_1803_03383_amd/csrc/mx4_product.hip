@@ -1,44 +1,264 @@
 // Products of MX4 matrices on the matrix cores: c = a b^T (+ c).
+//
+// A workgroup makes a tile of c.  Stages of 256 values of K (128 bytes of codes and 8 scales a row) of both
+// operands go to LDS by global_load_lds, double-buffered; a wave reads fragments of 32 rows and multiplies
+// them with v_mfma_scale_f32_32x32x64_f8f6f4 in 4 bits (the 16x16x128 form sustains 5.1 - 5.9
+// PFLOP/s on random codes, this one 6.8, where the power limit holds it).  The order of K within a stage
+// is free as long as both operands have the same: lane half h takes the four blocks of group h of a row,
+// so that its scales of the stage are one word and the instruction picks the byte.  16-byte pieces of
+// a row are permuted in LDS (piece p of row r lies at p ^ r / 2 % 8), so that the 16 rows that are read at once
+// cover every bank once; the permutation is made on the source address.
+#include <cmath>
+
 #include "halp_internal.hpp"
 #include "mx4.hpp"
 
 namespace halp {
 namespace {
 
+constexpr int kStage = 128;  // bytes of a row per stage: two groups of 128 values
+
 struct ProductArgs {
   MxView a, b;
   void* c;
   int64_t ldc;
   int accumulate;
+  int vec;         // c's rows can be written 16 bytes at a time
+  int tiles_m, tiles_n;
+  int cuts;        // parts of K; more than one: part z goes to rows z M and up of c
 };
 
-// v_mfma_scale_f32_16x16x128_f8f6f4, both operands in 4 bits: lane l holds row l % 16 and the block of 32
-// values l / 16 of a group of 128, with that block's scale in byte 0; the result's lane l holds
-// column l % 16 of rows 4 (l / 16) .. + 3.
-__device__ __forceinline__ v4f32 mfma4(uint4 a, uint4 b, v4f32 c, uint32_t sa, uint32_t sb) {
-  const v8i32 x{(int)a.x, (int)a.y, (int)a.z, (int)a.w}, y{(int)b.x, (int)b.y, (int)b.z, (int)b.w};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);
+// Lane l holds row l % 32 and block l / 32 of two of both operands, with that block's scale in byte SEL; the result's
+// lane l holds column l % 32 (a row of y) and rows 8 (i / 4) + 4 (l / 32) + i % 4 (rows of x), i = 0 .. 15.
+template <int SEL>
+__device__ __forceinline__ v16f32 mfma4(uint4 x, uint4 y, v16f32 c, uint32_t sx, uint32_t sy) {
+  // 4-bit operands are the first four registers
+  const v4i32 xv = __builtin_bit_cast(v4i32, x), yv = __builtin_bit_cast(v4i32, y);
+  const v8i32 p = __builtin_shufflevector(xv, xv, 0, 1, 2, 3, -1, -1, -1, -1), q = __builtin_shufflevector(yv, yv, 0, 1, 2, 3, -1, -1, -1, -1);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, c, 4, 4, SEL, (int)sx, SEL, (int)sy);
 }
 
-// One wave per 16 x 16 piece of c, operands straight from memory.  Rows past the end repeat the last one.
-template <typename T>
-__global__ __launch_bounds__(64) void product_tiles(ProductArgs a) {
-  const int lane = threadIdx.x, r = lane % 16, q = lane / 16;
-  const int64_t tn = (a.b.rows + 15) / 16, m0 = blockIdx.x / tn * 16, n0 = blockIdx.x % tn * 16;
-  const int64_t m = min(m0 + r, a.a.rows - 1), n = min(n0 + r, a.b.rows - 1);
-  const uint8_t *ca = a.a.codes + m * a.a.ldc + q * 16, *cb = a.b.codes + n * a.b.ldc + q * 16;
-  const uint8_t *sa = a.a.scales + m * a.a.lds + q, *sb = a.b.scales + n * a.b.lds + q;
-  v4f32 acc{};
-  for (int64_t g = 0; g < mx_groups(a.a.cols); ++g)
-    acc = mfma4(*reinterpret_cast<const uint4*>(ca + 64 * g), *reinterpret_cast<const uint4*>(cb + 64 * g), acc,
-                sa[4 * g], sb[4 * g]);
-  if (n0 + r >= a.b.rows) return;
+using LPtr = __attribute__((address_space(3))) void*;
+
+// 64 times 16 bytes from base + off (a lane's own, 32 bits) to LDS at `to` (bytes, a multiple of 1024 past the wave's
+// start) and up, lane after lane.  Issued by hand: the compiler takes the builtin for a store to all of LDS
+// and would have every later LDS read wait for it.  Complete after s_waitcnt vmcnt(0).  on: ~0 or 0, all lanes or none, so that
+// a load can be left out without a branch, which would part the products around it.  All lanes are active.
+__device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t off, uint32_t to, uint32_t on) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+               ::"s"(to), "v"(off), "s"(base), "s"(on));
+}
+
+// the same of 64 times 4 bytes, 256 in all
+__device__ __forceinline__ void word_to_lds(const uint8_t* base, uint32_t off, uint32_t to, uint32_t on) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1"
+               ::"s"(to), "v"(off), "s"(base), "s"(on));
+}
+
+// a pointer that is the same in every lane, in scalar registers
+__device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
+}
+
+// ROWS rows of one operand for a tile: where a lane loads from.  In LDS codes lie row after row, and so do scales.
+template <int ROWS, int THREADS>
+struct Source {
+  static constexpr int kPieces = ROWS * 8 / THREADS, kWords = ROWS * 2 / THREADS;
+  static constexpr int kLoads = kPieces + kWords;  // per lane and stage
+  static_assert(kPieces * THREADS == ROWS * 8 && kWords * THREADS == ROWS * 2, "");
+  const uint8_t *codes, *scales;
+  uint32_t off[kPieces], word[kWords];
+
+  __device__ __forceinline__ void init(const MxView& m, int64_t row0, int64_t stage0) {
+    codes = scalar(m.codes + row0 * m.ldc + stage0 * kStage);
+    scales = scalar(m.scales + row0 * m.lds + stage0 * 8);
+    // rows past the end repeat the last one; 256 rows of less than 2^23 bytes are within 32 bits
+    const uint32_t last = (uint32_t)min((int64_t)ROWS - 1, m.rows - 1 - row0);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t row = m0 + 4 * q + i;
-    if (row >= a.a.rows) break;
-    T* c = static_cast<T*>(a.c) + row * a.ldc + n0 + r;
-    *c = (T)(a.accumulate ? to_f32(*c) + acc[i] : acc[i]);
+    for (int i = 0; i < kPieces; ++i) {
+      const uint32_t p = i * THREADS + threadIdx.x, r = p / 8;
+      off[i] = min(r, last) * (uint32_t)m.ldc + 16 * ((p ^ r / 2) & 7);
+      asm volatile("" : "+v"(off[i]));  // one register: the compiler would keep the 64-bit multiply-add's two
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t w = i * THREADS + threadIdx.x;
+      word[i] = min(w / 2, last) * (uint32_t)m.lds + 4 * (w % 2);
+      asm volatile("" : "+v"(word[i]));
+    }
+  }
+  // load i of stage s to the buffers at LDS addresses c (codes) and k (scales).  half: the stage has one group only,
+  // which is read in place of the other.
+  __device__ __forceinline__ void fetch(int i, int64_t s, bool half, uint32_t c, uint32_t k, uint32_t on) const {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (i < kPieces) {
+      const uint32_t p = i * THREADS + threadIdx.x;
+      to_lds(scalar(codes + s * kStage), off[i] - (half ? 16 * ((p ^ (p / 16)) & 4) : 0), c + i * THREADS * 16 + wave * 1024, on);
+    } else {
+      i -= kPieces;
+      const uint32_t w = i * THREADS + threadIdx.x;
+      word_to_lds(scalar(scales + s * 8), word[i] - (half ? 4 * (w % 2) : 0), k + i * THREADS * 4 + wave * 256, on);
+    }
+  }
+};
+
+// Tiles of WM FM x WN FN fragments, one wave FM x FN of them.  A stage is four steps (block j of each group) of FM x FN
+// products.  A step's fragments are read during the step before; the barrier that a stage has arrived for
+// stands one step before its first product, when all of the stage before has been read, so that the
+// matrix cores do not wait for it.
+template <typename T, int WM, int WN, int FM, int FN>
+__global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
+  constexpr int kThreads = WM * WN * 64, BM = WM * FM * 32, BN = WN * FN * 32;
+  constexpr int kCodes = (BM + BN) * kStage, kBuffer = kCodes + (BM + BN) * 8;
+  __shared__ __align__(16) uint8_t lds[2 * kBuffer];
+
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 32, h = lane / 32;
+  const int wm = wave / WN, wn = wave % WN;
+  // workgroups go to the XCDs in turn: each XCD takes a run of tiles, in bands of eight tile rows
+  const int total = a.tiles_m * a.tiles_n, x = blockIdx.x % 8, i = blockIdx.x / 8;
+  const int tile = x * (total / 8) + min(x, total % 8) + i, cut = blockIdx.y;
+  const int band = tile / (8 * a.tiles_n), rest = tile % (8 * a.tiles_n), height = min(8, a.tiles_m - 8 * band);
+  const int64_t m0 = (int64_t)(8 * band + rest % height) * BM, n0 = (int64_t)(rest / height) * BN;
+
+  Source<BM, kThreads> sa;
+  Source<BN, kThreads> sb;
+  const int64_t groups = mx_groups(a.a.cols), all = (groups + 1) / 2;
+  const int first = (int)(all * cut / a.cuts), stages = (int)(all * (cut + 1) / a.cuts) - first;
+  const bool odd = (groups & 1) && cut == a.cuts - 1;  // the last stage has one group
+  sa.init(a.a, m0, first);
+  sb.init(a.b, n0, first);
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LPtr)lds;
+  constexpr int kLoads = sa.kLoads + sb.kLoads;
+  const auto fetch = [&](int i, int s) {  // load i of stage s
+    const uint32_t at = lds0 + (s & 1) * kBuffer;
+    const bool half = odd && s == stages - 1;
+    const uint32_t on = __builtin_amdgcn_readfirstlane(s < stages ? ~0u : 0u);
+    if (i < sa.kLoads) sa.fetch(i, s, half, at, at + kCodes, on);
+    else if (i < kLoads) sb.fetch(i - sa.kLoads, s, half, at + BM * kStage, at + kCodes + BM * 8, on);
+  };
+
+  v16f32 acc[FM][FN] = {};
+  uint4 fx[2][FM] = {}, fy[2][FN] = {};  // fragments by step
+  uint32_t sx[FM] = {}, sy[FN] = {};
+
+  // row m of the products of step j
+  const auto products = [&](auto step, int m) {
+    constexpr int j = decltype(step)::value;
+#pragma unroll
+    for (int n = 0; n < FN; ++n) acc[m][n] = mfma4<j>(fy[j % 2][n], fx[j % 2][m], acc[m][n], sy[n], sx[m]);
+  };
+
+  if (stages) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) fetch(i, 0);
+  }
+  for (int s = 0; s < stages; ++s) {
+    // this stage has arrived, and every wave has read the one before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const uint8_t* codes = lds + (s & 1) * kBuffer;
+    // Row m of the products of a step, with a part of the next step's reads and of the next stage's loads before it.
+    // The order is held: the compiler would put the reads behind the products, where they are waited for.
+    const auto part = [&](auto step, int j, int m) {  // j: the step that is read
+      const int piece = (((4 * h + j) ^ r / 2) & 7) * 16;
+#pragma unroll
+      for (int n = m * FN / FM; n < (m + 1) * FN / FM; ++n)
+        fy[j % 2][n] = *reinterpret_cast<const uint4*>(codes + BM * kStage + ((wn * FN + n) * 32 + r) * kStage + piece);
+      fx[j % 2][m] = *reinterpret_cast<const uint4*>(codes + ((wm * FM + m) * 32 + r) * kStage + piece);
+      constexpr int kPer = (kLoads + 3 * FM - 1) / (3 * FM);  // all in the first three steps
+#pragma unroll
+      for (int n = 0; n < kPer; ++n) fetch((j * FM + m) * kPer + n, s + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      products(step, m);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    uint32_t nx[FM], ny[FN];
+    const uint32_t* scales = reinterpret_cast<const uint32_t*>(codes + kCodes) + h;
+#pragma unroll
+    for (int m = 0; m < FM; ++m) nx[m] = scales[2 * ((wm * FM + m) * 32 + r)];
+#pragma unroll
+    for (int n = 0; n < FN; ++n) ny[n] = scales[2 * (BM + (wn * FN + n) * 32 + r)];
+#pragma unroll
+    for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 3>{}, 0, m);
+    // The group that an odd row's last stage lacks gets scales of 0 on both sides, 2^-254 together: what was read in
+    // its place adds nothing.
+    const bool none = s == stages - 1 && odd && h;
+#pragma unroll
+    for (int m = 0; m < FM; ++m) sx[m] = none ? 0 : nx[m];
+#pragma unroll
+    for (int n = 0; n < FN; ++n) sy[n] = none ? 0 : ny[n];
+#pragma unroll
+    for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 0>{}, 1, m);
+#pragma unroll
+    for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 1>{}, 2, m);
+#pragma unroll
+    for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 2>{}, 3, m);
+  }
+#pragma unroll
+  for (int m = 0; m < FM; ++m) products(std::integral_constant<int, 3>{}, m);
+
+  // 32 rows at a time through LDS (each wave its own part), so that rows leave in 16-byte pieces, whole lines
+  // together: straight from the accumulators a line would be written 8 bytes at a time.
+  constexpr int kPer = 16 / sizeof(T), kRow = FN * 32 + kPer, kPieces = FN * 32 / kPer;  // elements, pieces a row
+  static_assert(WM * WN * 32 * kRow * sizeof(T) <= sizeof lds, "");
+  asm volatile("s_barrier" ::: "memory");
+  T* own = reinterpret_cast<T*>(lds) + wave * 32 * kRow;
+#pragma unroll
+  for (int m = 0; m < FM; ++m) {
+    struct alignas(4 * sizeof(T)) Four { T v[4]; };
+    struct alignas(16) Piece { T v[kPer]; };
+#pragma unroll
+    for (int n = 0; n < FN; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        Four o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o.v[e] = (T)acc[m][n][4 * g + e];
+        *reinterpret_cast<Four*>(own + r * kRow + n * 32 + 8 * g + 4 * h) = o;
+      }
+#pragma unroll
+    for (int p = lane; p < 32 * kPieces; p += 64) {
+      Piece o = *reinterpret_cast<const Piece*>(own + p / kPieces * kRow + p % kPieces * kPer);
+      const int64_t row = m0 + (wm * FM + m) * 32 + p / kPieces, col = n0 + wn * FN * 32 + p % kPieces * kPer;
+      if (row >= a.a.rows) continue;
+      T* c = static_cast<T*>(a.c) + (cut * a.a.rows + row) * a.ldc + col;
+      if (a.vec && col + kPer <= a.b.rows) {
+        if (a.accumulate) {
+          const Piece before = *reinterpret_cast<const Piece*>(c);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) o.v[e] = (T)(to_f32(before.v[e]) + to_f32(o.v[e]));
+        }
+        *reinterpret_cast<Piece*>(c) = o;
+      } else {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          if (col + e < a.b.rows) c[e] = (T)(a.accumulate ? to_f32(c[e]) + to_f32(o.v[e]) : to_f32(o.v[e]));
+      }
+    }
+  }
+}
+
+struct JoinArgs {
+  const float* parts;  // [cuts][M][ldp]
+  void* c;
+  int64_t M, N, ldp, ldc;
+  int cuts, accumulate;
+};
+
+// c = the parts' sum in their order (+ c): four columns per thread
+template <typename T>
+__global__ __launch_bounds__(256) void join_cuts(JoinArgs a) {
+  const int64_t per = a.ldp / 4;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < a.M * per; i += gridDim.x * 256ll) {
+    const int64_t row = i / per, col = i % per * 4;
+    v4f32 sum = *reinterpret_cast<const v4f32*>(a.parts + row * a.ldp + col);
+    for (int z = 1; z < a.cuts; ++z) sum += *reinterpret_cast<const v4f32*>(a.parts + (z * a.M + row) * a.ldp + col);
+    T* c = static_cast<T*>(a.c) + row * a.ldc + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.N) c[e] = (T)(a.accumulate ? to_f32(c[e]) + sum[e] : sum[e]);
   }
 }
 
@@ -49,6 +269,14 @@ struct RowArgs {
   void* y;
   int64_t ldy;
 };
+
+// v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds row l % 16 and block l / 16 of four; the result's lane l holds column
+// l % 16 and rows 4 (l / 16) .. + 3.  Scales in byte 0.
+__device__ __forceinline__ v4f32 mfma4_rows(uint4 x, uint4 y, v4f32 c, uint32_t sx, uint32_t sy) {
+  const v4i32 xv = __builtin_bit_cast(v4i32, x), yv = __builtin_bit_cast(v4i32, y);
+  const v8i32 p = __builtin_shufflevector(xv, xv, 0, 1, 2, 3, -1, -1, -1, -1), q = __builtin_shufflevector(yv, yv, 0, 1, 2, 3, -1, -1, -1, -1);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 4, 4, 0, (int)sx, 0, (int)sy);
+}
 
 // One wave per 16 rows of w; a lane quantizes the block of x that it multiplies.
 template <typename X, typename Y>
@@ -76,7 +304,7 @@ __global__ __launch_bounds__(64) void row_product(RowArgs a) {
       const uint32_t c = mx_round_nearest(__builtin_bit_cast(float, bits & 0x7FFFFFFFu) * inv) | (bits >> 31) << 3;
       out[e / 8] |= (s == 255u ? 0u : c) << (4 * (e % 8));
     }
-    acc = mfma4(uint4{out[0], out[1], out[2], out[3]}, *reinterpret_cast<const uint4*>(cb + 64 * g), acc, s, sb[4 * g]);
+    acc = mfma4_rows(uint4{out[0], out[1], out[2], out[3]}, *reinterpret_cast<const uint4*>(cb + 64 * g), acc, s, sb[4 * g]);
   }
   if (n0 + r >= a.w.rows) return;
 #pragma unroll
@@ -88,15 +316,75 @@ __global__ __launch_bounds__(64) void row_product(RowArgs a) {
 
 }  // namespace
 
-int64_t mx4_product_workspace(int64_t, int64_t, int64_t, int) { return 0; }
+namespace {
 
-int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, int64_t ldc, bool accumulate, void*,
-                       int64_t, hipStream_t s) {
-  const int64_t tiles = (a.rows + 15) / 16 * ((b.rows + 15) / 16);
-  if (tiles >= int64_t(1) << 31) return HALP_ERR_UNSUPPORTED;
-  return with_type(type, [&](auto t) {
-    using T = decltype(t);
-    hipLaunchKernelGGL(product_tiles<T>, dim3((unsigned)tiles), dim3(64), 0, s, ProductArgs{a, b, c, ldc, accumulate});
+// How a product is made: the edge of its tiles (256, 128, 64: one, two, four workgroups to a CU) and the parts that K is
+// cut in.  Small tiles fill the CUs where there are few, at the price of more reads; parts cost a pass over
+// them.  The choice is the least of an estimate in microseconds fitted to timings on this GPU: a stage takes 2.0
+// with 256-tiles on every CU (1.2 with a few: the power limit), 0.9 and 1.5 with one and two 128-tiles
+// on a CU, 0.55 to 1.2 with one to four 64-tiles; beginning and ending a tile 12, 4 and 2.2.  On both sides of its
+// borders (measured, us): 4096 x 4096 x 2048 29 / 34 / 49 with 256 / 128 / 64, 4096 x 2048 x 4096 34 / 28 / 47,
+// 300 x 4096 x 4096 26 / 15 / 13; 1000 x 784 x 60000 with 128 in 1, 2, 4, 8, 16 parts 231, 126, 74, 69, 78.
+struct Plan {
+  int tile, cuts;
+};
+
+Plan plan(int64_t M, int64_t N, int64_t K, int cus) {
+  const int64_t stages = (mx_groups(K) + 1) / 2;
+  const auto stage_us = [&](int tile, double per_cu) {  // workgroups per CU
+    const int n = (int)std::ceil(per_cu);
+    if (tile == 256) return 1.2 + 0.8 * (per_cu < 1 ? per_cu : 1);
+    if (tile == 128) return n == 1 ? 0.9 : 1.5;
+    return n == 1 ? 0.55 : n == 2 ? 0.75 : n == 3 ? 1.0 : 1.2;
+  };
+  Plan best{128, 1};
+  double least = 1e300;
+  for (int tile = 256, most = 1; tile >= 64; tile /= 2, most *= 2)
+    for (int cuts = 1; cuts == 1 || (cuts <= 16 && stages / cuts >= 4); cuts *= 2) {
+      const double blocks = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * cuts / cus;  // per CU
+      const double ends = tile == 256 ? 12 : tile == 128 ? 4 : 2.2, full = std::floor(blocks / most), rest = blocks - full * most;
+      const double length = (double)((stages + cuts - 1) / cuts);
+      double us = full * (length * stage_us(tile, most) + ends);
+      if (rest > 0) us += length * stage_us(tile, rest) + ends;
+      if (cuts > 1) us += 3.5 + (double)cuts * M * N * 8 / 6e6;
+      if (us < least) least = us, best = Plan{tile, cuts};
+    }
+  return best;
+}
+
+int64_t parts_stride(int64_t N) { return (N + 3) / 4 * 4; }
+
+}  // namespace
+
+int64_t mx4_product_workspace(int64_t M, int64_t N, int64_t K, int cus) {
+  const Plan p = plan(M, N, K, cus);
+  return p.cuts > 1 ? sizeof(float) * p.cuts * M * parts_stride(N) : 0;
+}
+
+int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, int64_t ldc, bool accumulate,
+                       void* workspace, int64_t workspace_bytes, int cus, hipStream_t s) {
+  Plan p = plan(a.rows, b.rows, a.cols, cus);
+  if (workspace_bytes < mx4_product_workspace(a.rows, b.rows, a.cols, cus)) p.cuts = 1;
+  const int64_t t = p.tile, tm = (a.rows + t - 1) / t, tn = (b.rows + t - 1) / t;
+  if (tm * tn >= int64_t(1) << 31 || tn >= int64_t(1) << 27) return HALP_ERR_UNSUPPORTED;
+  const auto tiles = [&](auto kind, void* out, int64_t ld, bool add) {
+    using T = decltype(kind);
+    const int vec = ld * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
+    const ProductArgs args{a, b, out, ld, add, vec, (int)tm, (int)tn, p.cuts};
+    const dim3 grid((unsigned)(tm * tn), (unsigned)p.cuts);
+    if (p.tile == 256) hipLaunchKernelGGL((product_tiles<T, 2, 4, 4, 2>), grid, dim3(512), 0, s, args);
+    else if (p.tile == 128) hipLaunchKernelGGL((product_tiles<T, 2, 2, 2, 2>), grid, dim3(256), 0, s, args);
+    else hipLaunchKernelGGL((product_tiles<T, 1, 2, 2, 1>), grid, dim3(128), 0, s, args);
+    return hip_ok(hipGetLastError());
+  };
+  return with_type(type, [&](auto kind) {
+    using T = decltype(kind);
+    if (p.cuts == 1) return tiles(T{}, c, ldc, accumulate);
+    const int64_t ldp = parts_stride(b.rows);
+    if (const int rc = tiles(float{}, workspace, ldp, false)) return rc;
+    const int64_t blocks = (a.rows * (ldp / 4) + 255) / 256;
+    hipLaunchKernelGGL(join_cuts<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s,
+                       JoinArgs{static_cast<const float*>(workspace), c, a.rows, b.rows, ldp, ldc, p.cuts, accumulate});
     return hip_ok(hipGetLastError());
   });
 }

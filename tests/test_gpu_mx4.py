@@ -168,6 +168,25 @@ def test_sums_that_are_representable_are_exact(M, N, K, cut):
     assert np.array_equal(c.double().cpu().numpy(), want + keep.double().cpu().numpy())
 
 
+@pytest.mark.parametrize("M,N,K", [(4200, 4000, 900), (4097, 4111, 130), (2100, 2300, 1300), (2049, 4097, 4230), (1030, 900, 9100)])
+def test_large_products_are_exact(M, N, K):
+    """Sizes at which each tile shape is taken, alone and cut: scales 1, so that sums of up to 36 K in quarters stay
+    whole numbers below 2^24 and both the product and torch's in 64 bits are exact."""
+    assert 36 * 4 * K < 2 ** 24
+    a, av = _random(M, K, 15, spread=0)
+    b, bv = _random(N, K, 16, spread=0)
+    want = torch.from_numpy(av).cuda() @ torch.from_numpy(bv).cuda().t()
+    for cut in (False, True):
+        for dtype in (torch.float32, torch.bfloat16):
+            out = torch.full((M, N + 8), 5.0, dtype=dtype, device="cuda")
+            _product(a, b, out[:, :N], cut=cut)
+            assert torch.equal(out[:, :N], want.float().to(dtype))
+            assert (out[:, N:] == 5).all()
+    c = torch.ones(M, N, device="cuda")
+    _product(a, b, c, add=True, cut=True)
+    assert torch.equal(c, want.float() + 1)
+
+
 def _bound(av, bv, dtype, want):
     """K roundings of a sum of K products, each at most a step of the sum of magnitudes, and the type's rounding."""
     sums = av.shape[1] * 2.0 ** -23 * np.abs(av).dot(np.abs(bv).T)

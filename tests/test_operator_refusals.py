@@ -19,7 +19,7 @@ def _mx(rows=8, cols=200, **kw):
 BAD_MATRIX = [(dict(rows=-1), hp.ERR_INVALID), (dict(rows=2 ** 31), hp.ERR_INVALID), (dict(codes=None), hp.ERR_NULL),
               (dict(scales=None), hp.ERR_NULL), (dict(ldc=112), hp.ERR_INVALID), (dict(ldc=136), hp.ERR_ALIGN),
               (dict(lds=4), hp.ERR_INVALID), (dict(lds=10), hp.ERR_ALIGN), (dict(codes=FAKE + 8), hp.ERR_ALIGN),
-              (dict(scales=FAKE + 2), hp.ERR_ALIGN), (dict(ldc=2 ** 40), hp.ERR_INVALID)]
+              (dict(scales=FAKE + 2), hp.ERR_ALIGN), (dict(ldc=2 ** 23), hp.ERR_INVALID), (dict(lds=2 ** 23), hp.ERR_INVALID)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_MATRIX)
