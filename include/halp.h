@@ -414,8 +414,9 @@ int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type
 int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes); /* on the current device */
 
 /* y[M][N] = Q(x)[M][K] w[N][K]^T for 0 <= M <= 16 rows of x in `xtype`, quantized to the nearest on the
- * way (the values halp_mx4_quantize gives): a served token's product in one launch.  Larger M:
- * HALP_ERR_UNSUPPORTED, quantize x and take halp_mx4_product.                                  */
+ * way (the values halp_mx4_quantize gives): a served token's product in one launch (two or more where the
+ * rows hold more than about 100 000 values together).  Larger M, or K > 131072: HALP_ERR_UNSUPPORTED,
+ * quantize x and take halp_mx4_product.  y must not overlap x or w.                           */
 int halp_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, const halp_mx4* w, void* y,
                          int32_t ytype, int64_t ldy, void* stream);
 

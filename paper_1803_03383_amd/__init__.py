@@ -324,36 +324,63 @@ def debug_step_latency(waves, steps, blocks, out=None, stream=None):
 
 # ---- operators without a handle: 4-bit microscaled matrices, AdamW ---------------------------
 
-_TYPES = {"torch.float32": TYPE_F32, "torch.bfloat16": TYPE_BF16, "torch.float16": TYPE_F16}
+_torch = None
+_TYPES = {}
+
+
+def _load_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _TYPES.update({torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16})
+        _torch = torch
+    return _torch
 
 
 def _type(t, what):
-    code = _TYPES.get(str(t.dtype))
+    _load_torch()
+    code = _TYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"{what}: float32, bfloat16 or float16 expected, not {t.dtype}")
     return code
 
 
-def _matrix(t, what, shape=None):
+def _matrix(t, what, rows=None, cols=None):
     """A 2-D tensor with unit stride along its rows; returns its row stride."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a 2-D tensor with unit stride along its rows expected")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(shape)} expected, not {tuple(t.shape)}")
-    # the stride of a single row is whatever torch has it be
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    if t.dim() != 2:
+        raise ValueError(f"{what}: a 2-D tensor expected")
+    (m, n), (ld, one) = t.shape, t.stride()
+    if n > 1 and one != 1:
+        raise ValueError(f"{what}: a unit stride along the rows expected")
+    if rows is not None and (m != rows or n != cols):
+        raise ValueError(f"{what}: shape ({rows}, {cols}) expected, not ({m}, {n})")
+    return ld if m > 1 else max(n, 1)  # the stride of a single row is whatever torch has it be
 
 
-def _on(stream, *tensors):
-    """The device the tensors share, made current for the call, and the stream: its current one unless given."""
-    import torch
-    dev = tensors[0].device
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
+def _same_device(t, *others):
+    """The index of the GPU that all tensors are on."""
+    dev = t.device
+    for o in others:
+        if o is not None and o.device != dev:
+            raise ValueError(f"tensors on {dev} and {o.device}")
     if dev.type != "cuda":
         raise ValueError(f"GPU tensors expected, not {dev}")
-    return torch.cuda.device(dev), C.c_void_p(torch.cuda.current_stream(dev).cuda_stream if stream is None else int(stream))
+    return dev.index
+
+
+def _run(name, dev, stream, *args):
+    """Calls the library with device `dev` current, on the stream given or on that device's current one."""
+    torch = _load_torch()
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    f = getattr(lib(), name)
+    if torch._C._cuda_getDevice() == dev:
+        rc = f(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = f(*args, stream)
+    if rc != 0:
+        raise HalpError(rc, name)
 
 
 class Mx4:
@@ -361,7 +388,8 @@ class Mx4:
     groups = ceil(cols / 128)."""
 
     def __init__(self, codes, scales, cols):
-        if str(codes.dtype) != "torch.uint8" or str(scales.dtype) != "torch.uint8":
+        torch = _load_torch()
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
             raise ValueError("codes and scales are uint8 tensors")
         groups = (cols + 127) // 128
         ldc, lds = _matrix(codes, "codes"), _matrix(scales, "scales")
@@ -373,11 +401,12 @@ class Mx4:
         # a single row has no stride to speak of: whole groups
         self.c = Mx4Struct(codes.data_ptr(), ldc if self.rows > 1 else 64 * groups, scales.data_ptr(),
                            lds if self.rows > 1 else 4 * groups, self.rows, cols)
+        self.ref = C.byref(self.c)
 
 
 def mx4_empty(rows, cols, device="cuda"):
     """Allocates an Mx4 whose contents are not set."""
-    import torch
+    torch = _load_torch()
     groups = (cols + 127) // 128
     return Mx4(torch.empty((rows, 64 * groups), dtype=torch.uint8, device=device),
                torch.empty((rows, 4 * groups), dtype=torch.uint8, device=device), cols)
@@ -385,21 +414,15 @@ def mx4_empty(rows, cols, device="cuda"):
 
 def mx4_quantize(x, q=None, qt=None, rounding=ROUND_NEAREST, seed=0, epoch=0, stream=None):
     """x [rows, cols] into q (Mx4 of its rows) and qt (Mx4 of its transpose), whichever are given."""
-    ldx = _matrix(x, "x")
-    given = [t for m in (q, qt) if m is not None for t in (m.codes, m.scales)]
-    dev, s = _on(stream, x, *given)
-    with dev:
-        _check(lib().halp_mx4_quantize(_ptr(x), _type(x, "x"), x.shape[0], x.shape[1], ldx,
-                                       None if q is None else C.byref(q.c), None if qt is None else C.byref(qt.c),
-                                       rounding, seed & (2 ** 64 - 1), epoch, s), "halp_mx4_quantize")
+    dev = _same_device(x, q and q.codes, qt and qt.codes)
+    _run("halp_mx4_quantize", dev, stream, x.data_ptr(), _type(x, "x"), x.shape[0], x.shape[-1], _matrix(x, "x"),
+         q and q.ref, qt and qt.ref, rounding, seed & (2 ** 64 - 1), epoch)
 
 
 def mx4_dequantize(q, out, stream=None):
     """The values of q into out [rows, cols]."""
-    ldo = _matrix(out, "out", (q.rows, q.cols))
-    dev, s = _on(stream, out, q.codes)
-    with dev:
-        _check(lib().halp_mx4_dequantize(C.byref(q.c), _ptr(out), _type(out, "out"), ldo, s), "halp_mx4_dequantize")
+    ldo = _matrix(out, "out", q.rows, q.cols)
+    _run("halp_mx4_dequantize", _same_device(out, q.codes), stream, q.ref, out.data_ptr(), _type(out, "out"), ldo)
 
 
 def mx4_product_workspace(M, N, K):
@@ -410,24 +433,23 @@ def mx4_product_workspace(M, N, K):
 
 
 def mx4_product(a, b, out, accumulate=False, workspace=None, stream=None):
-    """out [M, N] = a [M, K] b [N, K]^T, added to out where accumulate is set; workspace: a uint8 tensor or None."""
-    ldc = _matrix(out, "out", (a.rows, b.rows))
-    dev, s = _on(stream, out, a.codes, b.codes, workspace)
-    if workspace is not None and not workspace.is_contiguous():
-        raise ValueError("workspace: a contiguous tensor expected")
-    with dev:
-        _check(lib().halp_mx4_product(C.byref(a.c), C.byref(b.c), _ptr(out), _type(out, "out"), ldc, int(bool(accumulate)),
-                                      _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                      s), "halp_mx4_product")
+    """out [M, N] = a [M, K] b [N, K]^T, added to out where accumulate is set; workspace: a contiguous tensor or None."""
+    ldc = _matrix(out, "out", a.rows, b.rows)
+    dev = _same_device(out, a.codes, b.codes, workspace)
+    at, room = None, 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor expected")
+        at, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _run("halp_mx4_product", dev, stream, a.ref, b.ref, out.data_ptr(), _type(out, "out"), ldc, 1 if accumulate else 0, at, room)
 
 
 def mx4_row_product(x, w, out, stream=None):
     """out [M, N] = x [M, K], quantized to the nearest on the way, times w [N, K]^T; M <= 16."""
-    ldx, ldy = _matrix(x, "x", (x.shape[0], w.cols)), _matrix(out, "out", (x.shape[0], w.rows))
-    dev, s = _on(stream, x, w.codes, out)
-    with dev:
-        _check(lib().halp_mx4_row_product(_ptr(x), _type(x, "x"), x.shape[0], ldx, C.byref(w.c), _ptr(out),
-                                          _type(out, "out"), ldy, s), "halp_mx4_row_product")
+    M = x.shape[0]
+    ldx, ldy = _matrix(x, "x", M, w.cols), _matrix(out, "out", M, w.rows)
+    _run("halp_mx4_row_product", _same_device(x, w.codes, out), stream, x.data_ptr(), _type(x, "x"), M, ldx, w.ref,
+         out.data_ptr(), _type(out, "out"), ldy)
 
 
 class AdamW:
@@ -437,34 +459,36 @@ class AdamW:
     narrower type).  The handle keeps references to them."""
 
     def __init__(self, tensors, state_bits=32, seed=0):
+        torch = _load_torch()
         self._h = C.c_void_p()
         tensors = [dict(t) for t in tensors]
         if not tensors:
             raise ValueError("at least one tensor expected")
         self._keep = tensors
-        state, dev = ("torch.float32" if state_bits == 32 else "torch.uint8"), tensors[0]["p"].device
+        state, dev = (torch.float32 if state_bits == 32 else torch.uint8), tensors[0]["p"].device
         copies = {_type(t["copy"], "copy") for t in tensors if t.get("copy") is not None}
         grads = {_type(t["g"], "g") for t in tensors}
         if len(grads) > 1 or len(copies) > 1:
             raise ValueError("all g have one type, and all copy")
+        want = {"p": torch.float32, "g": None, "copy": None, "m": state, "v": state}
+        if state_bits == 8:
+            want |= {"m_scale": torch.uint8, "v_scale": torch.uint8}
         arr = (AdamWTensor * len(tensors))()
         for a, t in zip(arr, tensors):
             a.n = t["p"].numel()
-            want = {"p": "torch.float32", "g": None, "copy": None, "m": state, "v": state}
-            if state_bits == 8:
-                want |= {"m_scale": "torch.uint8", "v_scale": "torch.uint8"}
             for name, dtype in want.items():
                 x = t.get(name)
                 if x is None:
                     if name != "copy":
                         raise ValueError(f"{name} is missing")
                     continue
-                if (dtype is not None and str(x.dtype) != dtype) or not x.is_contiguous() or x.device != dev:
+                if (dtype is not None and x.dtype != dtype) or not x.is_contiguous() or x.device != dev:
                     raise ValueError(f"{name}: a contiguous {dtype or 'floating-point'} tensor on {dev} expected")
                 if x.numel() != ((a.n + 31) // 32 if name.endswith("_scale") else a.n):
                     raise ValueError(f"{name}: {x.numel()} elements for a tensor of {a.n}")
                 setattr(a, name, x.data_ptr())
-        with _on(None, tensors[0]["p"])[0]:
+        self._dev = _same_device(tensors[0]["p"])
+        with torch.cuda.device(self._dev):
             _check(lib().halp_adamw_create(C.byref(self._h), arr, len(tensors), state_bits, grads.pop(),
                                            copies.pop() if copies else TYPE_BF16, seed & (2 ** 64 - 1)), "halp_adamw_create")
 
@@ -484,33 +508,37 @@ class AdamW:
         """One step.  step counts from 1; step_at (int64) and lr_at (float32), one-element GPU tensors, take the place of
         step and lr where given; grad_scale (float32, one element) scales the gradients and skips the step where it
         is not finite."""
-        for name, t, dtype in (("grad_scale", grad_scale, "torch.float32"), ("step_at", step_at, "torch.int64"),
-                               ("lr_at", lr_at, "torch.float32")):
-            if t is not None and (str(t.dtype) != dtype or t.numel() != 1):
+        at = []
+        for name, t, dtype in (("step_at", step_at, _torch.int64), ("lr_at", lr_at, _torch.float32),
+                               ("grad_scale", grad_scale, _torch.float32)):
+            if t is None:
+                at.append(None)
+                continue
+            if t.dtype != dtype or t.numel() != 1:
                 raise ValueError(f"{name}: one {dtype} expected")
-        a = AdamWArgs(lr, beta1, beta2, eps, weight_decay, step, _ptr(step_at), _ptr(lr_at), _ptr(grad_scale))
-        dev, s = _on(stream, self._keep[0]["p"], grad_scale, step_at, lr_at)
-        with dev:
-            _check(lib().halp_adamw_step(self._h, C.byref(a), s), "halp_adamw_step")
+            if _same_device(t) != self._dev:
+                raise ValueError(f"{name}: on {t.device}, the tensors on cuda:{self._dev}")
+            at.append(t.data_ptr())
+        a = AdamWArgs(lr, beta1, beta2, eps, weight_decay, step, *at)
+        _run("halp_adamw_step", self._dev, stream, self._h, C.byref(a))
 
     def grad_norm(self, max_norm, out, stream=None):
         """out (float32 [2]): the norm of all gradients, and the grad_scale that clips it to max_norm."""
-        if str(out.dtype) != "torch.float32" or out.numel() != 2 or not out.is_contiguous():
+        if out.dtype != _torch.float32 or out.numel() != 2 or not out.is_contiguous():
             raise ValueError("out: two contiguous float32 expected")
-        dev, s = _on(stream, self._keep[0]["p"], out)
-        with dev:
-            _check(lib().halp_adamw_grad_norm(self._h, max_norm, _ptr(out), s), "halp_adamw_grad_norm")
+        if _same_device(out) != self._dev:
+            raise ValueError(f"out: on {out.device}, the tensors on cuda:{self._dev}")
+        _run("halp_adamw_grad_norm", self._dev, stream, self._h, max_norm, out.data_ptr())
 
 
 def adamw_read_moments(m, m_scale, v, v_scale, m_out, v_out, stream=None):
     """The values of 8-bit states (uint8 codes and scales) as float32."""
-    n = m.numel()
-    for name, t, dtype, k in (("m", m, "torch.uint8", n), ("m_scale", m_scale, "torch.uint8", (n + 31) // 32),
-                              ("v", v, "torch.uint8", n), ("v_scale", v_scale, "torch.uint8", (n + 31) // 32),
-                              ("m_out", m_out, "torch.float32", n), ("v_out", v_out, "torch.float32", n)):
-        if str(t.dtype) != dtype or t.numel() != k or not t.is_contiguous():
-            raise ValueError(f"{name}: {k} contiguous {dtype} expected")
-    dev, s = _on(stream, m, m_scale, v, v_scale, m_out, v_out)
-    with dev:
-        _check(lib().halp_adamw_read_moments(_ptr(m), _ptr(m_scale), _ptr(v), _ptr(v_scale), n, _ptr(m_out), _ptr(v_out), s),
-               "halp_adamw_read_moments")
+    torch, n = _load_torch(), m.numel()
+    k = (n + 31) // 32
+    for name, t, dtype, count in (("m", m, torch.uint8, n), ("m_scale", m_scale, torch.uint8, k), ("v", v, torch.uint8, n),
+                                  ("v_scale", v_scale, torch.uint8, k), ("m_out", m_out, torch.float32, n),
+                                  ("v_out", v_out, torch.float32, n)):
+        if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+            raise ValueError(f"{name}: {count} contiguous {dtype} expected")
+    _run("halp_adamw_read_moments", _same_device(m, m_scale, v, v_scale, m_out, v_out), stream, m.data_ptr(), m_scale.data_ptr(),
+         v.data_ptr(), v_scale.data_ptr(), n, m_out.data_ptr(), v_out.data_ptr())

@@ -105,7 +105,9 @@ int halp_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, c
   if (rc != HALP_OK) return rc;
   if (M > 16) return HALP_ERR_UNSUPPORTED;
   if (M == 0 || w->rows == 0) return HALP_OK;
-  return launch_mx4_row_product(x, xtype, M, ldx, mx_view(*w), y, ytype, ldy, as_stream(stream));
+  int cus = 0;
+  if ((rc = count_cus(&cus)) != HALP_OK) return rc;
+  return launch_mx4_row_product(x, xtype, M, ldx, mx_view(*w), y, ytype, ldy, cus, as_stream(stream));
 }
 
 }  // extern "C"

@@ -262,58 +262,6 @@ __global__ __launch_bounds__(256) void join_cuts(JoinArgs a) {
   }
 }
 
-struct RowArgs {
-  const void* x;
-  int64_t M, ldx;
-  MxView w;
-  void* y;
-  int64_t ldy;
-};
-
-// v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds row l % 16 and block l / 16 of four; the result's lane l holds column
-// l % 16 and rows 4 (l / 16) .. + 3.  Scales in byte 0.
-__device__ __forceinline__ v4f32 mfma4_rows(uint4 x, uint4 y, v4f32 c, uint32_t sx, uint32_t sy) {
-  const v4i32 xv = __builtin_bit_cast(v4i32, x), yv = __builtin_bit_cast(v4i32, y);
-  const v8i32 p = __builtin_shufflevector(xv, xv, 0, 1, 2, 3, -1, -1, -1, -1), q = __builtin_shufflevector(yv, yv, 0, 1, 2, 3, -1, -1, -1, -1);
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 4, 4, 0, (int)sx, 0, (int)sy);
-}
-
-// One wave per 16 rows of w; a lane quantizes the block of x that it multiplies.
-template <typename X, typename Y>
-__global__ __launch_bounds__(64) void row_product(RowArgs a) {
-  const int lane = threadIdx.x, r = lane % 16, q = lane / 16;
-  const int64_t n0 = blockIdx.x * 16ll, n = min(n0 + r, a.w.rows - 1);
-  const X* x = static_cast<const X*>(a.x) + min((int64_t)r, a.M - 1) * a.ldx;
-  const uint8_t *cb = a.w.codes + n * a.w.ldc + q * 16, *sb = a.w.scales + n * a.w.lds + q;
-  v4f32 acc{};
-  for (int64_t g = 0; g < mx_groups(a.w.cols); ++g) {
-    const int64_t k0 = g * kMxGroup + q * kMxBlock;
-    float v[kMxBlock];
-    uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < kMxBlock; ++e) {
-      v[e] = k0 + e < a.w.cols ? to_f32(x[k0 + e]) : 0.f;
-      most = max(most, __builtin_bit_cast(uint32_t, v[e]) & 0x7FFFFFFFu);
-    }
-    const uint32_t s = mx_scale(most);
-    const float inv = mx_inverse(s);
-    uint32_t out[4] = {};
-#pragma unroll
-    for (int e = 0; e < kMxBlock; ++e) {
-      const uint32_t bits = __builtin_bit_cast(uint32_t, v[e]);
-      const uint32_t c = mx_round_nearest(__builtin_bit_cast(float, bits & 0x7FFFFFFFu) * inv) | (bits >> 31) << 3;
-      out[e / 8] |= (s == 255u ? 0u : c) << (4 * (e % 8));
-    }
-    acc = mfma4_rows(uint4{out[0], out[1], out[2], out[3]}, *reinterpret_cast<const uint4*>(cb + 64 * g), acc, s, sb[4 * g]);
-  }
-  if (n0 + r >= a.w.rows) return;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t row = 4 * q + i;
-    if (row < a.M) static_cast<Y*>(a.y)[row * a.ldy + n0 + r] = (Y)acc[i];
-  }
-}
-
 }  // namespace
 
 namespace {
@@ -386,19 +334,6 @@ int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, 
     hipLaunchKernelGGL(join_cuts<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s,
                        JoinArgs{static_cast<const float*>(workspace), c, a.rows, b.rows, ldp, ldc, p.cuts, accumulate});
     return hip_ok(hipGetLastError());
-  });
-}
-
-int launch_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, const MxView& w, void* y,
-                           int32_t ytype, int64_t ldy, hipStream_t s) {
-  return with_type(xtype, [&](auto xt) {
-    return with_type(ytype, [&](auto yt) {
-      using X = decltype(xt);
-      using Y = decltype(yt);
-      hipLaunchKernelGGL((row_product<X, Y>), dim3((unsigned)((w.rows + 15) / 16)), dim3(64), 0, s,
-                         RowArgs{x, M, ldx, w, y, ldy});
-      return hip_ok(hipGetLastError());
-    });
   });
 }
 
