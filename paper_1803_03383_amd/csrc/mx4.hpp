@@ -49,29 +49,8 @@ __device__ __forceinline__ float mx_scale_value(uint32_t s) {
   return __builtin_bit_cast(float, s == 255u ? 0x7FC00000u : (s ? s << 23 : 0x400000u));
 }
 
-// |x| 2^(127 - s) = t in [0, 6] to a code.  The step is 1/2, 1 or 2 for t below 2, 4 and 6.
-__device__ __forceinline__ uint32_t mx_round_nearest(float t) {
-  const int k = t >= 4.f ? 2 : (t >= 2.f ? 1 : 0);
-  return (uint32_t)__builtin_rintf(ldexpf(t, 1 - k)) + 2u * k;  // half way: the even multiple is the even code
-}
-
-// the same, up where the fraction of t / step is at least (511 - 2 r) / 512, r in [0, 256): the
-// comparison is one of integers, since only whole 512ths of the fraction matter
-__device__ __forceinline__ uint32_t mx_round_stochastic(float t, uint32_t r) {
-  const uint32_t z = (uint32_t)(t * 1024.f);
-  const uint32_t k = z >= 4096u ? 2u : (z >= 2048u ? 1u : 0u);
-  return (((z >> k) + 2u * r + 1u) >> 9) + 2u * k;
-}
-
-// value of a code without its scale
-__device__ __forceinline__ float mx_code_value(uint32_t c) {
-  const uint32_t m = c & 7u;
-  // 0 and .5 by hand, the others: exponent m / 2 - 1, mantissa bit m % 2
-  const uint32_t bits = m < 2u ? (m ? 0x3F000000u : 0u) : ((m >> 1) + 126u) << 23 | (m & 1u) << 22;
-  return __builtin_bit_cast(float, bits | (c & 8u) << 28);
-}
-
 // ---- 16 bytes of values in one lane: four floats, or eight of 16 bits ------------------------------
+using v2f32 = float __attribute__((ext_vector_type(2)));
 using v2u16 = unsigned short __attribute__((ext_vector_type(2)));
 
 // the values from p on (any alignment of T), n of them, zeros behind
@@ -169,7 +148,7 @@ inline bool type_known(int32_t type) { return type >= HALP_TYPE_F32 && type <= H
 
 // launchers; arguments have been checked
 int launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, const MxView* q,
-                        const MxView* qt, int32_t rounding, uint64_t seed, uint32_t epoch, hipStream_t s);
+                        const MxView* qt, int32_t rounding, uint64_t seed, uint32_t epoch, int cus, hipStream_t s);
 int launch_mx4_dequantize(const MxView& q, void* out, int32_t type, int64_t ldo, hipStream_t s);
 int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, int64_t ldc, bool accumulate,
                        void* workspace, int64_t workspace_bytes, int cus, hipStream_t s);

@@ -58,8 +58,10 @@ int halp_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, i
   MxView v, vt;
   if (q) v = mx_view(*q);
   if (qt) vt = mx_view(*qt);
+  int cus = 0;
+  if ((rc = count_cus(&cus)) != HALP_OK) return rc;
   return launch_mx4_quantize(x, type, rows, cols, ldx, q ? &v : nullptr, qt ? &vt : nullptr, rounding, seed,
-                             (uint32_t)epoch, as_stream(stream));
+                             (uint32_t)epoch, cus, as_stream(stream));
 }
 
 int halp_mx4_dequantize(const halp_mx4* q, void* out, int32_t type, int64_t ldo, void* stream) {
