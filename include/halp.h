@@ -448,7 +448,8 @@ typedef struct { /* DEVICE pointers of one tensor of n contiguous elements (n >=
 } halp_adamw_tensor;
 
 typedef struct {
-  double lr, beta1, beta2, eps, weight_decay; /* lr >= 0, 0 <= beta < 1, eps > 0, weight_decay >= 0 */
+  double lr, beta1, beta2, eps, weight_decay; /* lr >= 0, 0 <= beta < 1, 2^-126 <= eps < 2^126,
+                             weight_decay >= 0                                                  */
   int64_t step;           /* t, 1 <= t < 2^32                                                  */
   const int64_t* step_at; /* DEVICE, or NULL: t is read there instead (a step captured into a
                              graph; the caller counts it up).  A t out of range skips the step */

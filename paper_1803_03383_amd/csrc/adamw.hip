@@ -10,7 +10,8 @@ namespace halp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;      // elements of one tensor that a workgroup takes at a time
+constexpr int kParts = 4;         // groups of four elements that a lane takes at a time
+constexpr int kChunk = 4 * kThreads * kParts;  // elements of one tensor that a workgroup takes at a time
 constexpr int kNormParts = 2048;  // partial sums of the gradient norm at most
 
 struct Tensor {
@@ -21,7 +22,8 @@ struct Tensor {
 
 struct StepArgs {
   const Tensor* tensors;
-  int64_t count, chunks;
+  const int32_t* owner;  // of each chunk, its tensor
+  int64_t chunks;
   double lr, beta1, beta2, decay;
   float eps;
   int64_t step;
@@ -30,16 +32,6 @@ struct StepArgs {
   const float* grad_scale;
   uint64_t seed;
 };
-
-__device__ __forceinline__ const Tensor& tensor_of(const Tensor* t, int64_t count, int64_t chunk) {
-  int64_t lo = 0, hi = count;  // the last tensor whose first chunk is not past this one
-  while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (t[mid].first <= chunk) lo = mid;
-    else hi = mid;
-  }
-  return t[lo];
-}
 
 // beta^t by repeated squaring, in 64 bits
 __device__ double power(double beta, uint64_t t) {
@@ -59,28 +51,38 @@ __device__ __forceinline__ uint32_t state_scale(uint32_t max_bits) {
   return max_bits >= 0x7F800000u ? 255u : (uint32_t)(s > 0 ? s : 0);
 }
 
-// a >= 0 times 2^(127 - s) in the format, rounded up or down by 16 random bits: what lies below the
-// third mantissa bit carries into it with its own probability.  A number below the least normal one
+// a >= 0 times 2^(127 - s) in the format, rounded up or down by 16 random bits (u, shifted left by 4): what lies below
+// the third mantissa bit carries into it with its own probability.  A number below the least normal one
 // has a fixed step, that of the least binade, and is moved there by adding its first number.
 template <int BIAS>
 __device__ __forceinline__ uint32_t state_code(float a, float inv, uint32_t u) {
   constexpr float kLeast = BIAS == 7 ? 0x1p-6f : 0x1p-14f;
+  constexpr uint32_t kZero = (127u - BIAS) << 23;  // bits of the format's exponent 0
   const float t = a * inv;
   const bool low = t < kLeast;
   const uint32_t bits = __builtin_bit_cast(uint32_t, low ? t + kLeast : t);
-  return ((bits + 16u * u + 8u) >> 20) - 8u * (127 - BIAS) - (low ? 8u : 0u);
+  return (bits + u - (low ? kZero + (1u << 23) - 8u : kZero - 8u)) >> 20;
 }
 
-__device__ __forceinline__ float read_m(uint32_t c, uint32_t s) {  // c: one byte
-  const uint32_t f = c & 7u, e = c >> 3 & 15u;
-  const float a = e ? __builtin_bit_cast(float, (e + 120u) << 23 | f << 20) : (float)f * 0x1p-9f;
-  return s == 255u ? __builtin_nanf("") : ldexpf(c & 128u ? -a : a, (int)s - 127);
+// The values of four codes of m: an 8-bit format of the hardware.
+__device__ __forceinline__ void read_m4(uint32_t c, uint32_t s, float* m) {
+  const float scale = mx_scale_value(s);
+  const v2f32 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+  m[0] = a.x * scale;
+  m[1] = a.y * scale;
+  m[2] = b.x * scale;
+  m[3] = b.y * scale;
 }
 
-__device__ __forceinline__ float read_v(uint32_t c, uint32_t s) {
-  const uint32_t f = c & 7u, e = c >> 3;
-  const float a = e ? __builtin_bit_cast(float, (e + 112u) << 23 | f << 20) : (float)f * 0x1p-17f;
-  return s == 255u ? __builtin_nanf("") : ldexpf(a, (int)s - 127);
+// ... and of v: the upper bits of a 16-bit float without its sign
+__device__ __forceinline__ void read_v4(uint32_t c, uint32_t s, float* v) {
+  const float scale = mx_scale_value(s);
+  const v2f16 a = __builtin_bit_cast(v2f16, __builtin_amdgcn_perm(0, c, 0x0C010C00u) << 7),
+              b = __builtin_bit_cast(v2f16, __builtin_amdgcn_perm(0, c, 0x0C030C02u) << 7);
+  v[0] = (float)a.x * scale;
+  v[1] = (float)a.y * scale;
+  v[2] = (float)b.x * scale;
+  v[3] = (float)b.y * scale;
 }
 
 // largest of eight adjacent lanes
@@ -96,14 +98,17 @@ struct alignas(4 * sizeof(T)) Four {
   T v[4];
 };
 
+// k of them from element e on; whole: all four, aligned
 template <typename T>
 __device__ __forceinline__ Four<T> load4(const void* p, int64_t e, int k, bool whole) {
   const T* at = static_cast<const T*>(p) + e;
-  Four<T> r{};
-  if (whole) return *reinterpret_cast<const Four<T>*>(at);
+  Four<T> r;
+  if (whole) {
+    r = *reinterpret_cast<const Four<T>*>(at);
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < k) r.v[i] = at[i];
+    for (int i = 0; i < 4; ++i) r.v[i] = i < k ? at[i] : T(0);
+  }
   return r;
 }
 
@@ -119,9 +124,18 @@ __device__ __forceinline__ void store4(void* p, int64_t e, int k, bool whole, co
     if (i < k) at[i] = r.v[i];
 }
 
-// Four consecutive elements per lane, eight lanes to a block of 8-bit states.
+// sqrt(v) within a step and a reciprocal within one: v_sqrt_f32 takes subnormal numbers for zero, so small ones are scaled
+__device__ __forceinline__ float fast_sqrt(float v) {
+  const bool small = v < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p96f : v);
+  return small ? r * 0x1p-48f : r;
+}
+
+// Four consecutive elements per lane, eight lanes to a block of 8-bit states.  Bound by memory with 32-bit states (5.3 TB/s
+// of 240 M elements, where a copy of 2 GB runs at 4.9); with 8-bit states the random blocks and the conversions take about
+// as long as the memory (4.1 TB/s of 100 M, and 5.3 with gradients in fp32 and a copy, in the same time).
 template <typename G, typename C, bool BITS8>
-__global__ __launch_bounds__(kThreads) void adamw_step(StepArgs a) {
+__global__ __launch_bounds__(kThreads, BITS8 ? 4 : 2) void adamw_step(StepArgs a) {
   const float scale = a.grad_scale ? *a.grad_scale : 1.f;
   if (!(fabsf(scale) < __builtin_inff())) return;
   const int64_t step = a.step_at ? *a.step_at : a.step;
@@ -131,78 +145,100 @@ __global__ __launch_bounds__(kThreads) void adamw_step(StepArgs a) {
               root = (float)(1 / sqrt(1 - power(a.beta2, step))), b1 = (float)a.beta1, b2 = (float)a.beta2,
               n1 = (float)(1 - a.beta1), n2 = (float)(1 - a.beta2);
   for (int64_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-    const Tensor& d = tensor_of(a.tensors, a.count, chunk);
+    const Tensor& d = a.tensors[a.owner[chunk]];
     const halp_adamw_tensor t = d.t;
     const uint64_t seed = a.seed + (uint64_t)(&d - a.tensors);
-    for (int part = 0; part < kChunk; part += 4 * kThreads) {
-      const int64_t e = (chunk - d.first) * kChunk + part + 4 * threadIdx.x;
-      if (e - 4 * threadIdx.x >= t.n) break;
-      const int k = (int)(t.n - e < 4 ? (t.n - e > 0 ? t.n - e : 0) : 4);  // elements of this lane
-      const bool whole = d.whole && k == 4;
-      Four<float> p = load4<float>(t.p, e, k, whole), m, v;
-      const Four<G> g = load4<G>(t.g, e, k, whole);
-      if (BITS8) {
-        const Four<uint8_t> mc = load4<uint8_t>(t.m, e, k, whole), vc = load4<uint8_t>(t.v, e, k, whole);
-        const uint32_t ms = k ? t.m_scale[e / 32] : 0, vs = k ? t.v_scale[e / 32] : 0;
+    const int64_t e0 = (chunk - d.first) * kChunk + 4 * threadIdx.x;
+    const auto run = [&](auto all) {  // all: every lane has its four, aligned
+      // everything is asked for before any of it is used
+      Four<float> p[kParts], m[kParts], v[kParts];
+      Four<G> g[kParts];
+      uint32_t mc[kParts], vc[kParts], ms[kParts], vs[kParts];
+      const auto elements = [&](int u) { return all ? 4 : (int)max((int64_t)0, min((int64_t)4, t.n - e0 - u * 4 * kThreads)); };
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        const int64_t e = e0 + u * 4 * kThreads;
+        const int k = elements(u);
+        const bool whole = all || (d.whole && k == 4);
+        p[u] = load4<float>(t.p, e, k, whole);
+        g[u] = load4<G>(t.g, e, k, whole);
+        if constexpr (BITS8) {
+          mc[u] = __builtin_bit_cast(uint32_t, load4<uint8_t>(t.m, e, k, whole));
+          vc[u] = __builtin_bit_cast(uint32_t, load4<uint8_t>(t.v, e, k, whole));
+          ms[u] = k ? t.m_scale[e / 32] : 0;
+          vs[u] = k ? t.v_scale[e / 32] : 0;
+        } else {
+          m[u] = load4<float>(t.m, e, k, whole);
+          v[u] = load4<float>(t.v, e, k, whole);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        const int64_t e = e0 + u * 4 * kThreads;
+        const int k = elements(u);
+        const bool whole = all || (d.whole && k == 4);
+        if (!all && e - 4 * threadIdx.x >= t.n) break;  // the same for all lanes
+        if constexpr (BITS8) {
+          read_m4(mc[u], ms[u], m[u].v);
+          read_v4(vc[u], vs[u], v[u].v);
+        }
+        uint32_t mmax = 0, vmax = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          m.v[i] = read_m(mc.v[i], ms);
-          v.v[i] = read_v(vc.v[i], vs);
+          const float gs = (float)g[u].v[i] * scale;
+          float &mi = m[u].v[i], &vi = v[u].v[i], &pi = p[u].v[i];
+          mi = mi * b1 + gs * n1;
+          vi = vi * b2 + (gs * gs) * n2;
+          pi = pi * keep - rate * (mi * __builtin_amdgcn_rcpf(fast_sqrt(vi) * root + a.eps));
+          if (BITS8 && (all || i < k)) {
+            mmax = max(mmax, __builtin_bit_cast(uint32_t, mi) & 0x7FFFFFFFu);
+            vmax = max(vmax, __builtin_bit_cast(uint32_t, vi) & 0x7FFFFFFFu);
+          }
         }
-      } else {
-        m = load4<float>(t.m, e, k, whole);
-        v = load4<float>(t.v, e, k, whole);
-      }
-      uint32_t mmax = 0, vmax = 0;
+        store4(t.p, e, k, whole, p[u]);
+        if (t.copy) {
+          Four<C> c;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float gs = (float)g.v[i] * scale;
-        m.v[i] = m.v[i] * b1 + gs * n1;
-        v.v[i] = v.v[i] * b2 + (gs * gs) * n2;
-        p.v[i] = p.v[i] * keep - rate * (m.v[i] / (sqrtf(v.v[i]) * root + a.eps));
-        if (i < k) {
-          mmax = max(mmax, __builtin_bit_cast(uint32_t, m.v[i]) & 0x7FFFFFFFu);
-          vmax = max(vmax, __builtin_bit_cast(uint32_t, v.v[i]) & 0x7FFFFFFFu);
+          for (int i = 0; i < 4; ++i) c.v[i] = (C)p[u].v[i];
+          store4(t.copy, e, k, whole, c);
         }
-      }
-      store4(t.p, e, k, whole, p);
-      if (t.copy) {
-        Four<C> c;
+        if constexpr (BITS8) {
+          const uint32_t sm = state_scale<7>(max_of_8(mmax)), sv = state_scale<15>(max_of_8(vmax));
+          const float im = mx_inverse(sm), iv = mx_inverse(sv);
+          const U4 r = stream_block(seed, kMoments, (uint32_t)step, (uint64_t)e / 4);
+          uint32_t cm = 0, cv = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c.v[i] = (C)p.v[i];
-        store4(t.copy, e, k, whole, c);
-      }
-      if (BITS8) {
-        const uint32_t ms = state_scale<7>(max_of_8(mmax)), vs = state_scale<15>(max_of_8(vmax));
-        const float mi = mx_inverse(ms), vi = mx_inverse(vs);
-        const U4 r = stream_block(seed, kMoments, (uint32_t)step, (uint64_t)e / 4);
-        Four<uint8_t> mc, vc;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t u = pick(r, i), bits = __builtin_bit_cast(uint32_t, m.v[i]);
-          const uint32_t cm = state_code<7>(__builtin_bit_cast(float, bits & 0x7FFFFFFFu), mi, u & 0xFFFFu) | (bits >> 24 & 128u);
-          const uint32_t cv = state_code<15>(v.v[i], vi, u >> 16);
-          mc.v[i] = (uint8_t)(ms == 255u ? 0u : cm);
-          vc.v[i] = (uint8_t)(vs == 255u ? 0u : cv);
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = pick(r, i);
+            const float mi = m[u].v[i];
+            const uint32_t sign = __builtin_bit_cast(uint32_t, mi) >> 31 << 7;
+            cm |= ((state_code<7>(fabsf(mi), im, (w & 0xFFFFu) << 4) & 127u) | sign) << (8 * i);
+            cv |= (state_code<15>(v[u].v[i], iv, w >> 16 << 4) & 255u) << (8 * i);
+          }
+          if (sm == 255u) cm = 0;
+          if (sv == 255u) cv = 0;
+          store4(t.m, e, k, whole, __builtin_bit_cast(Four<uint8_t>, cm));
+          store4(t.v, e, k, whole, __builtin_bit_cast(Four<uint8_t>, cv));
+          if (k && threadIdx.x % 8 == 0) {
+            t.m_scale[e / 32] = (uint8_t)sm;
+            t.v_scale[e / 32] = (uint8_t)sv;
+          }
+        } else {
+          store4(t.m, e, k, whole, m[u]);
+          store4(t.v, e, k, whole, v[u]);
         }
-        store4(t.m, e, k, whole, mc);
-        store4(t.v, e, k, whole, vc);
-        if (k && threadIdx.x % 8 == 0) {
-          t.m_scale[e / 32] = (uint8_t)ms;
-          t.v_scale[e / 32] = (uint8_t)vs;
-        }
-      } else {
-        store4(t.m, e, k, whole, m);
-        store4(t.v, e, k, whole, v);
       }
-    }
+    };
+    if (d.whole && (chunk - d.first + 1) * kChunk <= t.n) run(std::true_type{});
+    else run(std::false_type{});
   }
 }
 
 // ---- norm of all gradients --------------------------------------------------------------------
 struct NormArgs {
   const Tensor* tensors;
-  int64_t count, chunks;
+  const int32_t* owner;
+  int64_t chunks;
   double* parts;
   int used;
   double most;
@@ -222,19 +258,30 @@ __device__ __forceinline__ double block_sum(double v) {  // in thread 0
 
 template <typename G>
 __global__ __launch_bounds__(kThreads) void norm_parts(NormArgs a) {
-  double sum = 0;
+  double sums[4] = {};
   for (int64_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-    const Tensor& d = tensor_of(a.tensors, a.count, chunk);
-    for (int part = 0; part < kChunk; part += 4 * kThreads) {
-      const int64_t e = (chunk - d.first) * kChunk + part + 4 * threadIdx.x;
-      if (e >= d.t.n) break;
-      const int k = (int)(d.t.n - e < 4 ? d.t.n - e : 4);
-      const Four<G> g = load4<G>(d.t.g, e, k, d.whole && k == 4);
+    const Tensor& d = a.tensors[a.owner[chunk]];
+    const int64_t e0 = (chunk - d.first) * kChunk + 4 * threadIdx.x;
+    Four<G> g[kParts];
+    if (d.whole && (chunk - d.first + 1) * kChunk <= d.t.n) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum += (double)(float)g.v[i] * (double)(float)g.v[i];
+      for (int u = 0; u < kParts; ++u) g[u] = load4<G>(d.t.g, e0 + u * 4 * kThreads, 4, true);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        const int64_t e = e0 + u * 4 * kThreads;
+        g[u] = load4<G>(d.t.g, e, (int)max((int64_t)0, min((int64_t)4, d.t.n - e)), false);
+      }
     }
+#pragma unroll
+    for (int u = 0; u < kParts; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double x = (double)(float)g[u].v[i];
+        sums[i] = __builtin_fma(x, x, sums[i]);
+      }
   }
-  sum = block_sum(sum);
+  const double sum = block_sum((sums[0] + sums[1]) + (sums[2] + sums[3]));
   if (threadIdx.x == 0) a.parts[blockIdx.x] = sum;
 }
 
@@ -252,12 +299,36 @@ struct ReadArgs {
   const uint8_t *m, *ms, *v, *vs;
   float *mo, *vo;
   int64_t n;
+  bool whole;
 };
 
 __global__ __launch_bounds__(kThreads) void read_moments(ReadArgs a) {
-  for (int64_t e = blockIdx.x * (int64_t)kThreads + threadIdx.x; e < a.n; e += gridDim.x * (int64_t)kThreads) {
-    a.mo[e] = read_m(a.m[e], a.ms[e / 32]);
-    a.vo[e] = read_v(a.v[e], a.vs[e / 32]);
+  for (int64_t chunk = blockIdx.x; chunk * kChunk < a.n; chunk += gridDim.x) {
+    const int64_t e0 = chunk * kChunk + 4 * threadIdx.x;
+    const auto run = [&](auto all) {
+      uint32_t mc[kParts], vc[kParts], ms[kParts], vs[kParts];
+      const auto elements = [&](int u) { return all ? 4 : (int)max((int64_t)0, min((int64_t)4, a.n - e0 - u * 4 * kThreads)); };
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        const int64_t e = e0 + u * 4 * kThreads;
+        const int k = elements(u);
+        mc[u] = __builtin_bit_cast(uint32_t, load4<uint8_t>(a.m, e, k, all));
+        vc[u] = __builtin_bit_cast(uint32_t, load4<uint8_t>(a.v, e, k, all));
+        ms[u] = k ? a.ms[e / 32] : 0;
+        vs[u] = k ? a.vs[e / 32] : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        const int64_t e = e0 + u * 4 * kThreads;
+        Four<float> m, v;
+        read_m4(mc[u], ms[u], m.v);
+        read_v4(vc[u], vs[u], v.v);
+        store4(a.mo, e, elements(u), all, m);
+        store4(a.vo, e, elements(u), all, v);
+      }
+    };
+    if (a.whole && (chunk + 1) * kChunk <= a.n) run(std::true_type{});
+    else run(std::false_type{});
   }
 }
 
@@ -280,9 +351,11 @@ unsigned grid_for(int64_t chunks, int64_t most) { return (unsigned)(chunks < mos
 using namespace halp;
 
 struct halp_adamw {
-  void* device_list = nullptr;  // Tensor [count], then the partial sums of the norm
+  void* workspace = nullptr;  // Tensor [count], the partial sums of the norm, the tensor of each chunk
+  const Tensor* tensors = nullptr;
   double* parts = nullptr;
-  int64_t count = 0, chunks = 0;
+  const int32_t* owner = nullptr;
+  int64_t chunks = 0;
   int bits = 32;
   int32_t grad_type = 0, copy_type = 0;
   uint64_t seed = 0;
@@ -299,39 +372,46 @@ int halp_adamw_create(halp_adamw** out, const halp_adamw_tensor* tensors, int64_
   if (state_bits != 8 && state_bits != 32) return HALP_ERR_UNSUPPORTED;
   for (int64_t i = 0; i < count; ++i)
     if (const int rc = check_tensor(tensors[i], state_bits, grad_type, copy_type)) return rc;
+  int64_t chunks = 0;
+  for (int64_t i = 0; i < count; ++i) chunks += (tensors[i].n + kChunk - 1) / kChunk;
+  const size_t list_bytes = sizeof(Tensor) * count, part_bytes = sizeof(double) * kNormParts, bytes = list_bytes + part_bytes + 4 * chunks;
   halp_adamw* h = new (std::nothrow) halp_adamw();
-  Tensor* list = new (std::nothrow) Tensor[count];
-  if (!h || !list) {
+  char* host = new (std::nothrow) char[bytes];
+  if (!h || !host) {
     delete h;
-    delete[] list;
+    delete[] host;
     return HALP_ERR_HIP;
   }
-  h->count = count; h->bits = state_bits; h->grad_type = grad_type; h->copy_type = copy_type; h->seed = seed;
+  h->chunks = chunks; h->bits = state_bits; h->grad_type = grad_type; h->copy_type = copy_type; h->seed = seed;
   const size_t state = state_bits == 8 ? 4 : 16;
+  int32_t* owner = reinterpret_cast<int32_t*>(host + list_bytes + part_bytes);
+  int64_t first = 0;
   for (int64_t i = 0; i < count; ++i) {
     const halp_adamw_tensor& t = tensors[i];
-    list[i].t = t;
-    list[i].first = h->chunks;
-    list[i].whole = aligned(t.p, 16) && aligned(t.g, 4 * type_bytes(grad_type)) && aligned(t.m, state) &&
-                    aligned(t.v, state) && aligned(t.copy, 4 * type_bytes(copy_type));
-    h->chunks += (t.n + kChunk - 1) / kChunk;
+    const Tensor d{t, first, aligned(t.p, 16) && aligned(t.g, 4 * type_bytes(grad_type)) && aligned(t.m, state) &&
+                                 aligned(t.v, state) && aligned(t.copy, 4 * type_bytes(copy_type))};
+    std::memcpy(host + sizeof(Tensor) * i, &d, sizeof d);
+    for (int64_t k = 0; k < (t.n + kChunk - 1) / kChunk; ++k) owner[first++] = (int32_t)i;
   }
-  const size_t bytes = sizeof(Tensor) * count;
-  const bool bad = hip_fail(hipMalloc(&h->device_list, bytes + sizeof(double) * kNormParts), "hipMalloc(adamw)") ||
-                   hip_fail(hipMemcpy(h->device_list, list, bytes, hipMemcpyHostToDevice), "hipMemcpy(adamw)");
-  delete[] list;
+  std::memset(host + list_bytes, 0, part_bytes);
+  const bool bad = hip_fail(hipMalloc(&h->workspace, bytes), "hipMalloc(adamw)") ||
+                   hip_fail(hipMemcpy(h->workspace, host, bytes, hipMemcpyHostToDevice), "hipMemcpy(adamw)");
+  delete[] host;
   if (bad) {
     halp_adamw_destroy(h);
     return HALP_ERR_HIP;
   }
-  h->parts = reinterpret_cast<double*>(static_cast<char*>(h->device_list) + bytes);
+  char* base = static_cast<char*>(h->workspace);
+  h->tensors = reinterpret_cast<const Tensor*>(base);
+  h->parts = reinterpret_cast<double*>(base + list_bytes);
+  h->owner = reinterpret_cast<const int32_t*>(base + list_bytes + part_bytes);
   *out = h;
   return HALP_OK;
 }
 
 int halp_adamw_destroy(halp_adamw* h) {
   if (!h) return HALP_ERR_NULL;
-  if (h->device_list) (void)hipFree(h->device_list);
+  if (h->workspace) (void)hipFree(h->workspace);
   delete h;
   return HALP_OK;
 }
@@ -339,12 +419,12 @@ int halp_adamw_destroy(halp_adamw* h) {
 int halp_adamw_step(halp_adamw* h, const halp_adamw_args* p, void* stream) {
   if (!h || !p) return HALP_ERR_NULL;
   if (!(p->lr >= 0) || !std::isfinite(p->lr) || !(p->beta1 >= 0 && p->beta1 < 1) || !(p->beta2 >= 0 && p->beta2 < 1) ||
-      !((float)p->eps > 0) || !std::isfinite((float)p->eps) || !(p->weight_decay >= 0) || !std::isfinite(p->weight_decay))
+      !((float)p->eps >= 0x1p-126f && (float)p->eps < 0x1p126f) || !(p->weight_decay >= 0) || !std::isfinite(p->weight_decay))
     return HALP_ERR_INVALID;
   if (!p->step_at && (p->step < 1 || p->step >= (int64_t(1) << 32))) return HALP_ERR_INVALID;
   if (!aligned(p->step_at, 8) || !aligned(p->lr_at, 4) || !aligned(p->grad_scale, 4)) return HALP_ERR_ALIGN;
   if (h->chunks == 0) return HALP_OK;
-  const StepArgs a{static_cast<const Tensor*>(h->device_list), h->count, h->chunks, p->lr, p->beta1, p->beta2,
+  const StepArgs a{h->tensors, h->owner, h->chunks, p->lr, p->beta1, p->beta2,
                    p->weight_decay, (float)p->eps, p->step, p->step_at, p->lr_at, p->grad_scale, h->seed};
   const dim3 grid(grid_for(h->chunks, int64_t(1) << 20));
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -363,7 +443,7 @@ int halp_adamw_grad_norm(halp_adamw* h, double max_norm, float* out, void* strea
   if (!h || !out) return HALP_ERR_NULL;
   if (!(max_norm > 0)) return HALP_ERR_INVALID;
   if (!aligned(out, 4)) return HALP_ERR_ALIGN;
-  NormArgs a{static_cast<const Tensor*>(h->device_list), h->count, h->chunks, h->parts, (int)grid_for(h->chunks, kNormParts),
+  NormArgs a{h->tensors, h->owner, h->chunks, h->parts, (int)grid_for(h->chunks, kNormParts),
              max_norm, out};
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return with_type(h->grad_type, [&](auto g) {
@@ -380,9 +460,10 @@ int halp_adamw_read_moments(const uint8_t* m, const uint8_t* m_scale, const uint
   if (n == 0) return HALP_OK;
   if (!m || !m_scale || !v || !v_scale || !m_out || !v_out) return HALP_ERR_NULL;
   if (!aligned(m_out, 4) || !aligned(v_out, 4)) return HALP_ERR_ALIGN;
-  const dim3 grid(grid_for((n + kThreads - 1) / kThreads, 65536));
+  const bool whole = aligned(m, 4) && aligned(v, 4) && aligned(m_out, 16) && aligned(v_out, 16);
+  const dim3 grid(grid_for((n + kChunk - 1) / kChunk, int64_t(1) << 20));
   hipLaunchKernelGGL(read_moments, grid, dim3(kThreads), 0, reinterpret_cast<hipStream_t>(stream),
-                     ReadArgs{m, m_scale, v, v_scale, m_out, v_out, n});
+                     ReadArgs{m, m_scale, v, v_scale, m_out, v_out, n, whole});
   return hip_ok(hipGetLastError());
 }
 

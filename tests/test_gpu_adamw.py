@@ -68,12 +68,13 @@ def _check(before, t, i, step, bits, seed, scale=1.0, hyper=HYPER):
             codes, scales = adamw.write(x, w, k)
             assert np.array_equal(new[k + "_scale"], scales)
             assert np.array_equal(new[k], codes)
-    # the update's errors: of m over the denominator, half of v's relative one, and eight roundings of its own
-    # (root, its factor and product, eps' sum, quotient, rate, product); p's: its factor, product and the difference
+    # the update's errors: of m over the denominator, half of v's relative one, and its own: the root and the reciprocal
+    # are within a step (two halves each), and six roundings (the root's factor and product, eps' sum, the reciprocal's
+    # product, rate, its product) make ten halves; p's: its factor, product and the difference
     rate, den = lr / (1 - b1 ** step), np.sqrt(v / (1 - b2 ** step)) + eps
     upd = rate * np.abs(m) / den
     rel_v = np.where(v > 0, dv / np.where(v > 0, v, 1), 0)
-    dp = rate * dm / den + upd * (8 * H + rel_v) + H * (2 * np.abs(old["p"]) + np.abs(p)) * 1.01
+    dp = rate * dm / den + upd * (10 * H + rel_v) + H * (2 * np.abs(old["p"]) + np.abs(p)) * 1.01
     assert (np.abs(new["p"] - p) <= dp).all()
     if "copy" in t:
         assert torch.equal(t["copy"].cpu(), t["p"].cpu().to(t["copy"].dtype))
