@@ -1,7 +1,7 @@
 // Products of MX4 matrices on the matrix cores: c = a b^T (+ c).
 //
 // A workgroup makes a tile of c.  Stages of 256 values of K (128 bytes of codes and 8 scales a row) of both
-// operands go to LDS by global_load_lds, double-buffered; a wave reads fragments of 32 rows and multiplies
+// operands go to LDS by global_load_lds, in two to four buffers; a wave reads fragments of 32 rows and multiplies
 // them with v_mfma_scale_f32_32x32x64_f8f6f4 in 4 bits (the 16x16x128 form sustains 5.1 - 5.9
 // PFLOP/s on random codes, this one 6.8, where the power limit holds it).  The order of K within a stage
 // is free as long as both operands have the same: lane half h takes the four blocks of group h of a row,
@@ -107,12 +107,12 @@ struct Source {
 // Tiles of WM FM x WN FN fragments, one wave FM x FN of them.  A stage is four steps (block j of each group) of FM x FN
 // products.  A step's fragments are read during the step before; the barrier that a stage has arrived for
 // stands one step before its first product, when all of the stage before has been read, so that the
-// matrix cores do not wait for it.
-template <typename T, int WM, int WN, int FM, int FN>
+// matrix cores do not wait for it.  D buffers: D - 1 stages are on their way or in use.
+template <typename T, int WM, int WN, int FM, int FN, int D>
 __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
   constexpr int kThreads = WM * WN * 64, BM = WM * FM * 32, BN = WN * FN * 32;
   constexpr int kCodes = (BM + BN) * kStage, kBuffer = kCodes + (BM + BN) * 8;
-  __shared__ __align__(16) uint8_t lds[2 * kBuffer];
+  __shared__ __align__(16) uint8_t lds[D * kBuffer];
 
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 32, h = lane / 32;
   const int wm = wave / WN, wn = wave % WN;
@@ -132,8 +132,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LPtr)lds;
   constexpr int kLoads = sa.kLoads + sb.kLoads;
-  const auto fetch = [&](int i, int s) {  // load i of stage s
-    const uint32_t at = lds0 + (s & 1) * kBuffer;
+  const auto fetch = [&](int i, int s, int buffer) {  // load i of stage s
+    const uint32_t at = lds0 + buffer * kBuffer;
     const bool half = odd && s == stages - 1;
     const uint32_t on = __builtin_amdgcn_readfirstlane(s < stages ? ~0u : 0u);
     if (i < sa.kLoads) sa.fetch(i, s, half, at, at + kCodes, on);
@@ -151,14 +151,17 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
     for (int n = 0; n < FN; ++n) acc[m][n] = mfma4<j>(fy[j % 2][n], fx[j % 2][m], acc[m][n], sy[n], sx[m]);
   };
 
-  if (stages) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) fetch(i, 0);
-  }
+  for (int s = 0; s < D - 1; ++s)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) fetch(i, s, s);
+  int buffer = 0, free = D - 1;  // of this stage; of the next one that is asked for
   for (int s = 0; s < stages; ++s) {
-    // this stage has arrived, and every wave has read the one before
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const uint8_t* codes = lds + (s & 1) * kBuffer;
+    // this stage has arrived (the loads of those behind it may be under way), and every wave has read the one before
+    static_assert((D - 2) * kLoads < 64, "");
+    if (D > 2 && s + D - 2 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const uint8_t* codes = lds + buffer * kBuffer;
     // Row m of the products of a step, with a part of the next step's reads and of the next stage's loads before it.
     // The order is held: the compiler would put the reads behind the products, where they are waited for.
     const auto part = [&](auto step, int j, int m) {  // j: the step that is read
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
       fx[j % 2][m] = *reinterpret_cast<const uint4*>(codes + ((wm * FM + m) * 32 + r) * kStage + piece);
       constexpr int kPer = (kLoads + 3 * FM - 1) / (3 * FM);  // all in the first three steps
 #pragma unroll
-      for (int n = 0; n < kPer; ++n) fetch((j * FM + m) * kPer + n, s + 1);
+      for (int n = 0; n < kPer; ++n) fetch((j * FM + m) * kPer + n, s + D - 1, free);
       __builtin_amdgcn_sched_barrier(0);
       products(step, m);
       __builtin_amdgcn_sched_barrier(0);
@@ -195,6 +198,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
     for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 1>{}, 2, m);
 #pragma unroll
     for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 2>{}, 3, m);
+    free = buffer;
+    buffer = buffer == D - 1 ? 0 : buffer + 1;
   }
 #pragma unroll
   for (int m = 0; m < FM; ++m) products(std::integral_constant<int, 3>{}, m);
@@ -203,7 +208,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
   // together: straight from the accumulators a line would be written 8 bytes at a time.
   constexpr int kPer = 16 / sizeof(T), kRow = FN * 32 + kPer, kPieces = FN * 32 / kPer;  // elements, pieces a row
   static_assert(WM * WN * 32 * kRow * sizeof(T) <= sizeof lds, "");
-  asm volatile("s_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   T* own = reinterpret_cast<T*>(lds) + wave * 32 * kRow;
 #pragma unroll
   for (int m = 0; m < FM; ++m) {
@@ -266,13 +271,13 @@ __global__ __launch_bounds__(256) void join_cuts(JoinArgs a) {
 
 namespace {
 
-// How a product is made: the edge of its tiles (256, 128, 64: one, two, four workgroups to a CU) and the parts that K is
+// How a product is made: the edge of its tiles (256, 128, 64: one, two, three workgroups to a CU) and the parts that K is
 // cut in.  Small tiles fill the CUs where there are few, at the price of more reads; parts cost a pass over
 // them.  The choice is the least of an estimate in microseconds fitted to timings on this GPU: a stage takes 2.0
-// with 256-tiles on every CU (1.2 with a few: the power limit), 0.9 and 1.5 with one and two 128-tiles
-// on a CU, 0.55 to 1.2 with one to four 64-tiles; beginning and ending a tile 12, 4 and 2.2.  On both sides of its
-// borders (measured, us): 4096 x 4096 x 2048 29 / 34 / 49 with 256 / 128 / 64, 4096 x 2048 x 4096 34 / 28 / 47,
-// 300 x 4096 x 4096 26 / 15 / 13; 1000 x 784 x 60000 with 128 in 1, 2, 4, 8, 16 parts 231, 126, 74, 69, 78.
+// with 256-tiles on every CU (1.2 with a few: the power limit), 0.78 and 1.5 with one and two 128-tiles
+// on a CU, 0.42 to 0.93 with one to three 64-tiles; beginning and ending a tile 12, 4 and 2.4.  On both sides of its
+// borders (measured, us): 4096 x 4096 x 2048 29 / 34 / 53 with 256 / 128 / 64, 4096 x 2048 x 4096 34 / 29 / 48,
+// 300 x 4096 x 4096 27 / 14 / 13; 1000 x 784 x 60000 with 128 in 1, 2, 4, 8, 16 parts 176, 100, 62, 69, 77.
 struct Plan {
   int tile, cuts;
 };
@@ -282,15 +287,15 @@ Plan plan(int64_t M, int64_t N, int64_t K, int cus) {
   const auto stage_us = [&](int tile, double per_cu) {  // workgroups per CU
     const int n = (int)std::ceil(per_cu);
     if (tile == 256) return 1.2 + 0.8 * (per_cu < 1 ? per_cu : 1);
-    if (tile == 128) return n == 1 ? 0.9 : 1.5;
-    return n == 1 ? 0.55 : n == 2 ? 0.75 : n == 3 ? 1.0 : 1.2;
+    if (tile == 128) return n == 1 ? 0.78 : 1.5;
+    return n == 1 ? 0.42 : n == 2 ? 0.7 : 0.93;
   };
   Plan best{128, 1};
   double least = 1e300;
-  for (int tile = 256, most = 1; tile >= 64; tile /= 2, most *= 2)
+  for (int tile = 256, most = 1; tile >= 64; tile /= 2, ++most)
     for (int cuts = 1; cuts == 1 || (cuts <= 16 && stages / cuts >= 4); cuts *= 2) {
       const double blocks = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * cuts / cus;  // per CU
-      const double ends = tile == 256 ? 12 : tile == 128 ? 4 : 2.2, full = std::floor(blocks / most), rest = blocks - full * most;
+      const double ends = tile == 256 ? 12 : tile == 128 ? 4 : 2.4, full = std::floor(blocks / most), rest = blocks - full * most;
       const double length = (double)((stages + cuts - 1) / cuts);
       double us = full * (length * stage_us(tile, most) + ends);
       if (rest > 0) us += length * stage_us(tile, rest) + ends;
@@ -320,9 +325,12 @@ int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, 
     const int vec = ld * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
     const ProductArgs args{a, b, out, ld, add, vec, (int)tm, (int)tn, p.cuts};
     const dim3 grid((unsigned)(tm * tn), (unsigned)p.cuts);
-    if (p.tile == 256) hipLaunchKernelGGL((product_tiles<T, 2, 4, 4, 2>), grid, dim3(512), 0, s, args);
-    else if (p.tile == 128) hipLaunchKernelGGL((product_tiles<T, 2, 2, 2, 2>), grid, dim3(256), 0, s, args);
-    else hipLaunchKernelGGL((product_tiles<T, 1, 2, 2, 1>), grid, dim3(128), 0, s, args);
+    if (p.tile == 256) hipLaunchKernelGGL((product_tiles<T, 2, 4, 4, 2, 2>), grid, dim3(512), 0, s, args);
+    // 128: two buffers let two workgroups share a CU; where each has one to itself, a third hides the loads' latency
+    // (1000 x 784 x 60000 in four parts 74 and 62 us, 4096 x 4096 x 4096 60 and 74)
+    else if (p.tile == 128 && tm * tn * p.cuts > cus) hipLaunchKernelGGL((product_tiles<T, 2, 2, 2, 2, 2>), grid, dim3(256), 0, s, args);
+    else if (p.tile == 128) hipLaunchKernelGGL((product_tiles<T, 2, 2, 2, 2, 3>), grid, dim3(256), 0, s, args);
+    else hipLaunchKernelGGL((product_tiles<T, 1, 2, 2, 1, 3>), grid, dim3(128), 0, s, args);
     return hip_ok(hipGetLastError());
   };
   return with_type(type, [&](auto kind) {
