@@ -2,8 +2,8 @@
 //
 // Bound by memory: x is read once for both forms.  A wave holds a tile of R rows and 1 KB of each in registers, 16
 // bytes of a row per lane.  A block of a row then lies in four (16-bit types) or eight (fp32) adjacent lanes,
-// a block of a column in one lane (R = 32), so that neither form moves values between waves or through LDS; four
-// waves take the four blocks of a stored group of the transposed form, 64 bytes of each of its rows.
+// a block of a column in one lane (R = 32), so that no values move between waves; four waves take the four blocks of
+// a stored group of the transposed form, and their codes meet in LDS to leave 64 bytes at a time.
 #include <utility>
 
 #include "halp_internal.hpp"
@@ -157,6 +157,12 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
   constexpr int kV = 16 / sizeof(T), kLanes = kMxBlock / kV;
   static_assert(!COLS || R == kMxBlock, "");
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  // The column blocks of the four waves meet here: blocks by value, lane and wave, the wave's place permuted so that lanes
+  // write to all banks (8192 x 8192 fp16 both ways 63 us without it and 54 with).  Not where they are rounded
+  // stochastically: the arithmetic bounds that, and the registers are needed (114 and 115).
+  constexpr bool kMeet = COLS && !RANDOM;
+  __shared__ uint4 out[kMeet ? 64 * kV * 4 : 1];
+  __shared__ __align__(4) uint8_t out_scales[kMeet ? 64 * kV * 4 : 4];
   const int forms = gridDim.y == 1 ? 3 : 1 << blockIdx.y;  // of a tile, by this workgroup
   for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
     const int64_t row0 = (t / a.across * 4 + wave) * R, col = (t % a.across * 64 + lane) * kV;
@@ -170,7 +176,7 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
       uint32_t kept = 0;  // of the lanes of a block, one keeps the scale of each row
       const auto one = [&](auto index) {
         constexpr int i = decltype(index)::value;
-        if (i >= there) return;
+        if (RANDOM && i >= there) return;
         // opaque, or the compiler would convert the values of all rows first, past the registers
         if constexpr (COLS && RANDOM && std::is_same_v<T, _Float16>) asm volatile("" : "+v"(x.v[i].x), "+v"(x.v[i].y), "+v"(x.v[i].z), "+v"(x.v[i].w));
         if (RANDOM && i % random.kRows == 0) random.make(a, row0 + i, col);
@@ -182,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
           else *reinterpret_cast<uint32_t*>(codes + i * a.q.ldc) = c;
         }
         if (lane % kLanes == i % kLanes) kept = s;
-        if (i % kLanes == kLanes - 1 || i == there - 1) {
+        if (i % kLanes == kLanes - 1 || i == (RANDOM ? there : R) - 1) {
           const int row = i / kLanes * kLanes + lane % kLanes;
           if (row <= i && row < rows) scales[row * a.q.lds] = (uint8_t)kept;
         }
@@ -244,11 +250,30 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
             c[g] = s == 255u ? 0u : d;
           }
         }
-        if (col + e < a.cols) {
+        if constexpr (kMeet) {
+          out[(e * 64 + lane) * 4 + (wave ^ (lane / 4 % 4))] = uint4{c[0], c[1], c[2], c[3]};
+          out_scales[(e * 64 + lane) * 4 + wave] = (uint8_t)s;
+        } else if (col + e < a.cols) {
           *reinterpret_cast<uint4*>(a.qt.codes + (col + e) * a.qt.ldc + 16 * block) = uint4{c[0], c[1], c[2], c[3]};
           a.qt.scales[(col + e) * a.qt.lds + block] = (uint8_t)s;
         }
       }
+      if constexpr (!kMeet) continue;
+      __syncthreads();
+      // the four waves' blocks of a column leave together, 64 bytes and a word of scales
+      const int64_t col0 = t % a.across * 64 * kV, group = t / a.across;
+#pragma unroll
+      for (int i = threadIdx.x; i < 64 * kV * 4; i += 256) {
+        const int n = i / 4, l = n / kV, e = n % kV;  // column n of the tile: value e of lane l
+        if (col0 + n < a.cols)
+          *reinterpret_cast<uint4*>(a.qt.codes + (col0 + n) * a.qt.ldc + 64 * group + 16 * (i % 4)) = out[(e * 64 + l) * 4 + (i % 4 ^ (l / 4 % 4))];
+      }
+#pragma unroll
+      for (int n = threadIdx.x; n < 64 * kV; n += 256)
+        if (col0 + n < a.cols)
+          *reinterpret_cast<uint32_t*>(a.qt.scales + (col0 + n) * a.qt.lds + 4 * group) =
+              *reinterpret_cast<const uint32_t*>(out_scales + (n % kV * 64 + n / kV) * 4);
+      __syncthreads();
     }
   }
 }
@@ -275,39 +300,43 @@ __global__ __launch_bounds__(256) void dequantize(ReadArgs a) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
     const int64_t row0 = (t / a.across * 4 + wave) * R, col = (t % a.across * 64 + lane) * kV, left = a.q.cols - col;
-    const int rows = left > 0 ? (int)min((int64_t)R, a.q.rows - row0) : 0;
     const uint8_t *codes = a.q.codes + row0 * a.q.ldc + col / 2, *scales = a.q.scales + row0 * a.q.lds + col / kMxBlock;
-    uint32_t c[R], s[R];
+    T* out = static_cast<T*>(a.out) + row0 * a.ldo + col;
+    const auto run = [&](auto all) {  // all: every lane has its values of every row
+      const int rows = all ? R : left > 0 ? (int)min((int64_t)R, a.q.rows - row0) : 0;
+      uint32_t c[R], s[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (i < rows) {
-        if constexpr (kV == 8) c[i] = *reinterpret_cast<const uint32_t*>(codes + i * a.q.ldc);
-        else c[i] = *reinterpret_cast<const uint16_t*>(codes + i * a.q.ldc);
-        s[i] = scales[i * a.q.lds];
+      for (int i = 0; i < R; ++i)
+        if (i < rows) {
+          if constexpr (kV == 8) c[i] = *reinterpret_cast<const uint32_t*>(codes + i * a.q.ldc);
+          else c[i] = *reinterpret_cast<const uint16_t*>(codes + i * a.q.ldc);
+          s[i] = scales[i * a.q.lds];
+        }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        if (i >= rows) break;
+        const float scale = mx_scale_value(s[i]);
+        float f[8];
+        read_two<0>(c[i], scale, f);
+        read_two<1>(c[i], scale, f + 2);
+        if constexpr (kV == 8) {
+          read_two<2>(c[i], scale, f + 4);
+          read_two<3>(c[i], scale, f + 6);
+        }
+        Piece o;
+#pragma unroll
+        for (int e = 0; e < kV; ++e) o.v[e] = (T)f[e];
+        if (all || left >= kV) {
+          *reinterpret_cast<Piece*>(out + i * a.ldo) = o;
+        } else {
+#pragma unroll
+          for (int e = 0; e < kV; ++e)
+            if (e < left) out[i * a.ldo + e] = o.v[e];
+        }
       }
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      if (i >= rows) break;
-      const float scale = mx_scale_value(s[i]);
-      float f[8];
-      read_two<0>(c[i], scale, f);
-      read_two<1>(c[i], scale, f + 2);
-      if constexpr (kV == 8) {
-        read_two<2>(c[i], scale, f + 4);
-        read_two<3>(c[i], scale, f + 6);
-      }
-      Piece o;
-#pragma unroll
-      for (int e = 0; e < kV; ++e) o.v[e] = (T)f[e];
-      T* out = static_cast<T*>(a.out) + (row0 + i) * a.ldo + col;
-      if (left >= kV) {
-        *reinterpret_cast<Piece*>(out) = o;
-      } else {
-#pragma unroll
-        for (int e = 0; e < kV; ++e)
-          if (e < left) out[e] = o.v[e];
-      }
-    }
+    };
+    if (row0 + R <= a.q.rows && __all(left >= kV)) run(std::true_type{});
+    else run(std::false_type{});
   }
 }
 
