@@ -19,6 +19,7 @@ using v8i32 = int __attribute__((ext_vector_type(8)));
 
 constexpr int kMxBlock = 32;   // values per scale
 constexpr int kMxGroup = 128;  // values per stored group: 64 bytes of codes, 4 scales
+constexpr int64_t kMxRowMost = 131072;  // columns of the row product: a row of x fits LDS
 
 inline __host__ __device__ int64_t mx_groups(int64_t cols) { return (cols + kMxGroup - 1) / kMxGroup; }
 

@@ -105,7 +105,7 @@ int halp_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, c
   if (rc == HALP_OK) rc = check_plain(x, xtype, M, w->cols, ldx);
   if (rc == HALP_OK) rc = check_plain(y, ytype, M, w->rows, ldy);
   if (rc != HALP_OK) return rc;
-  if (M > 16) return HALP_ERR_UNSUPPORTED;
+  if (M > 16 || w->cols > kMxRowMost) return HALP_ERR_UNSUPPORTED;
   if (M == 0 || w->rows == 0) return HALP_OK;
   int cus = 0;
   if ((rc = count_cus(&cus)) != HALP_OK) return rc;

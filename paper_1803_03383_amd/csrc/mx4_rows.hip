@@ -22,6 +22,8 @@ __host__ __device__ inline int64_t scale_row(int64_t chunks) { return 16 * chunk
 // sums of two units: one is read while the next is written
 __host__ __device__ inline int sum_bytes(int waves) { return 2 * waves * 64 * (int)sizeof(v4f32); }
 
+static_assert(kMostLds - 2 * kWaves * 64 * 16 >= (256 + 16) * (kMxRowMost / 512) + 20, "a row and the sums fit");
+
 struct RowArgs {
   const void* x;
   int64_t M, ldx;
@@ -150,7 +152,6 @@ int launch_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx,
   // half a chunk counted for a unit's own.  One row times 11000 x 5000 (688 tiles of ten chunks): 10.0 us with a
   // chunk a wave and unit (three units to a CU), 8.8 with two (one unit of 15 waves).
   const int64_t all = (w.rows + 15) / 16;
-  if (chunks > 256) return HALP_ERR_UNSUPPORTED;  // then a row of x fits LDS beside the sums
   int split = 1, tiles = 1;
   double least = 1e300;
   for (int64_t turn = (chunks + kWaves - 1) / kWaves; chunks && turn <= chunks; ++turn) {

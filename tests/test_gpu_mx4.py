@@ -168,7 +168,8 @@ def test_sums_that_are_representable_are_exact(M, N, K, cut):
     assert np.array_equal(c.double().cpu().numpy(), want + keep.double().cpu().numpy())
 
 
-@pytest.mark.parametrize("M,N,K", [(4200, 4000, 900), (4097, 4111, 130), (2100, 2300, 1300), (2049, 4097, 4230), (1030, 900, 9100)])
+@pytest.mark.parametrize("M,N,K", [(4200, 4000, 900), (4097, 4111, 130), (2100, 2300, 1300), (2049, 4097, 4230), (1030, 900, 9100),
+                                   (1700, 2000, 700), (2000, 1900, 500), (2000, 1900, 129), (1000, 784, 60000), (4090, 4000, 2400)])
 def test_large_products_are_exact(M, N, K):
     """Sizes at which each tile shape is taken, alone and cut: scales 1, so that sums of up to 36 K in quarters stay
     whole numbers below 2^24 and both the product and torch's in 64 bits are exact."""
@@ -267,6 +268,23 @@ def test_row_product(M, N, K, xtype, ytype):
     inside = np.abs(want) < torch.finfo(ytype).max
     assert (np.abs(got - want) <= _bound(xv, wv, ytype, want))[inside].all()
     assert (out[M:] == 3).all() and (out[:, N:] == 3).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(16, 70, 20_001), (3, 40, 131_072), (1, 33, 131_000), (16, 20_000, 1500), (2, 5000, 8192)])
+def test_row_product_of_long_rows_and_many(M, N, K):
+    """Rows that LDS does not hold at once, and more tiles than a workgroup takes in one turn."""
+    g = torch.Generator("cuda").manual_seed(K)
+    w, x = hp.mx4_empty(N, K), torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    hp.mx4_quantize(torch.randn(N, K, generator=g, device="cuda"), w)
+    q, xv, wv = hp.mx4_empty(M, K), torch.empty(M, K, device="cuda"), torch.empty(N, K, device="cuda")
+    hp.mx4_quantize(x, q)
+    hp.mx4_dequantize(q, xv)
+    hp.mx4_dequantize(w, wv)
+    out = torch.full((M + 1, N), 9.0, device="cuda")
+    hp.mx4_row_product(x, w, out[:M])
+    want = xv.double() @ wv.double().t()
+    bound = K * 2.0 ** -23 * (xv.double().abs() @ wv.double().abs().t()) + 2.0 ** -24 * want.abs()
+    assert ((out[:M] - want).abs() <= bound).all() and (out[M:] == 9).all()
 
 
 @pytest.mark.parametrize("offset", [1, 2, 5])
@@ -399,6 +417,24 @@ def test_another_stream_and_replayed_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(st[k], want[k]) for k in names), turn
+
+
+def test_a_workspace_that_is_too_small_is_left_alone():
+    a, av = _random(70, 9000, 17, spread=0)
+    b, bv = _random(90, 9000, 18, spread=0)
+    need = hp.mx4_product_workspace(70, 90, 9000)
+    assert need > 0  # this product is cut where it can be
+    ws = torch.full((need // 16 * 16 - 16,), 7, dtype=torch.uint8, device="cuda")
+    out = torch.empty(70, 90, device="cuda")
+    hp.mx4_product(a, b, out, workspace=ws)
+    assert np.array_equal(out.double().cpu().numpy(), av.dot(bv.T)) and (ws == 7).all()
+
+
+def test_a_matrix_times_itself():
+    a, av = _random(130, 700, 19, spread=0)
+    out = torch.empty(130, 130, device="cuda")
+    _product(a, a, out)
+    assert np.array_equal(out.double().cpu().numpy(), av.dot(av.T))
 
 
 def test_calls_repeat_their_bits():

@@ -79,6 +79,8 @@ def test_row_product():
         return L.halp_mx4_row_product(x, xt, M, ldx, C.byref(_mx()), y, yt, ldy, None)
 
     assert product(M=17) == hp.ERR_UNSUPPORTED
+    wide = _mx(cols=131073, ldc=65600, lds=4100)
+    assert L.halp_mx4_row_product(FAKE, 0, 1, 131073, C.byref(wide), FAKE, 0, 8, None) == hp.ERR_UNSUPPORTED
     assert product(x=None) == hp.ERR_NULL and product(y=None) == hp.ERR_NULL
     for kw in (dict(M=-1), dict(xt=3), dict(yt=-1), dict(ldx=199), dict(ldy=7)):
         assert product(**kw) == hp.ERR_INVALID, kw
