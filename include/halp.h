@@ -385,9 +385,9 @@ typedef struct {
   int64_t rows, cols; /* 0 <= rows < 2^31, 0 <= cols < 2^24                                    */
 } halp_mx4;
 
-/* x (DEVICE, rows of ldx >= cols elements of `type`, any alignment of its type) into MX4 with x
- * read once: q ([rows][cols], blocks along x's rows), qt ([cols][rows], the transpose, blocks
- * along x's columns), or both; either may be NULL.  rounding HALP_ROUND_STOCHASTIC: with r = 8
+/* x (DEVICE, rows of ldx >= cols elements of `type`, any alignment of its type) into MX4: q
+ * ([rows][cols], blocks along x's rows), qt ([cols][rows], the transpose, blocks along x's
+ * columns), or both in one launch; either may be NULL.  rounding HALP_ROUND_STOCHASTIC: with r = 8
  * bits of the stream of `seed` and `epoch` (0 <= epoch < 2^32), a value is rounded up where the
  * fraction of |x| / step is at least (511 - 2 r) / 512; element (i, j) of a form takes byte j % 16
  * of block i * ceil(cols / 16) + j / 16 of purpose 6 (q) or 7 (qt, in its own rows and columns).
@@ -408,7 +408,8 @@ int halp_mx4_dequantize(const halp_mx4* q, void* out, int32_t type, int64_t ldo,
  * K = 0 gives zeros.  workspace (DEVICE, 16-byte aligned, may be NULL): with at least
  * halp_mx4_product_workspace bytes, products with few tiles and a long K are cut along K and their parts joined in a
  * fixed order; without it the same products run uncut and end in another rounding.  Calls that
- * overlap in time must not share it.  c must not overlap the operands or the workspace.        */
+ * overlap in time must not share it.  c must not overlap the operands or the workspace.
+ * ceil(M / 64) ceil(N / 64) >= 2^25 - 3: HALP_ERR_UNSUPPORTED.                                 */
 int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type, int64_t ldc, int32_t accumulate,
                      void* workspace, int64_t workspace_bytes, void* stream);
 int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes); /* on the current device */

@@ -65,6 +65,6 @@ def write(x, words16, kind):
     return codes, scales
 
 
-def random_words(n, t, seed):
-    """The words of elements 0 .. n - 1 of a tensor with its own seed at step t."""
-    return philox_blocks(np.arange(-(-n // 4), dtype=np.uint64), t, 8, seed).reshape(-1)[:n]
+def random_words(n, t, seed, first=0):
+    """The words of elements first .. first + n - 1 (first a multiple of 4) of a tensor with its own seed at step t."""
+    return philox_blocks(first // 4 + np.arange(-(-n // 4), dtype=np.uint64), t, 8, seed).reshape(-1)[:n]

@@ -319,7 +319,6 @@ int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, 
   Plan p = plan(a.rows, b.rows, a.cols, cus);
   if (workspace_bytes < mx4_product_workspace(a.rows, b.rows, a.cols, cus)) p.cuts = 1;
   const int64_t t = p.tile, tm = (a.rows + t - 1) / t, tn = (b.rows + t - 1) / t;
-  if (tm * tn >= int64_t(1) << 31 || tn >= int64_t(1) << 27) return HALP_ERR_UNSUPPORTED;
   const auto tiles = [&](auto kind, void* out, int64_t ld, bool add) {
     using T = decltype(kind);
     const int vec = ld * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;

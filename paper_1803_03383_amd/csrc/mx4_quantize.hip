@@ -340,6 +340,9 @@ __global__ __launch_bounds__(256) void dequantize(ReadArgs a) {
   }
 }
 
+// a launch holds fewer than 2^32 threads: 256 for each of these workgroups
+unsigned grid_of(int64_t tiles) { return (unsigned)(tiles < (1 << 22) ? tiles : 1 << 22); }
+
 }  // namespace
 
 int launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, const MxView* q,
@@ -356,7 +359,7 @@ int launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols,
     a.tiles = a.across * ((rows + 4 * height - 1) / (4 * height));
     // Both forms of a tile by one workgroup, so that x is read once; by two, side by side, where that leaves no CU without
     // one: 300 x 4096 in bf16 10.2 us instead of 12.4, stochastically 17.8 instead of 25.9
-    const dim3 grid((unsigned)(a.tiles < (int64_t(1) << 24) ? a.tiles : int64_t(1) << 24), q && qt && a.tiles <= cus ? 2 : 1);
+    const dim3 grid(grid_of(a.tiles), q && qt && a.tiles <= cus ? 2 : 1);
     const auto launch = [&](auto with_rows, auto with_cols, auto is_random, auto tall) {
       hipLaunchKernelGGL((quantize_tiles<T, decltype(with_rows)::value, decltype(with_cols)::value, decltype(is_random)::value,
                                          decltype(tall)::value>), grid, dim3(256), 0, s, a);
@@ -380,7 +383,7 @@ int launch_mx4_dequantize(const MxView& q, void* out, int32_t type, int64_t ldo,
     using T = decltype(t);
     constexpr int64_t kWidth = 64 * 16 / sizeof(T);
     const int64_t across = (q.cols + kWidth - 1) / kWidth, tiles = across * ((q.rows + 31) / 32);
-    hipLaunchKernelGGL(dequantize<T>, dim3((unsigned)(tiles < (int64_t(1) << 24) ? tiles : int64_t(1) << 24)), dim3(256), 0, s,
+    hipLaunchKernelGGL(dequantize<T>, dim3(grid_of(tiles)), dim3(256), 0, s,
                        ReadArgs{q, out, ldo, across, tiles});
     return hip_ok(hipGetLastError());
   });

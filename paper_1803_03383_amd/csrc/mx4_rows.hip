@@ -171,7 +171,7 @@ int launch_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx,
         const int64_t rows = M - m < most ? M - m : most, lds = sum_bytes(waves) + rows * row;
         const int64_t a_cu = kMostLds / lds < kWaves / waves ? kMostLds / lds : kWaves / waves, held = cus * a_cu;
         if (hip_fail(hipFuncSetAttribute(reinterpret_cast<const void*>(row_product<X, Y>),
-                                         hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds), "hipFuncSetAttribute"))
+                                         hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds), "hipFuncSetAttribute"))
           return (int)HALP_ERR_HIP;
         hipLaunchKernelGGL((row_product<X, Y>), dim3((unsigned)(units < held ? units : held)), dim3(64 * waves), (size_t)lds, s,
                            RowArgs{static_cast<const X*>(x) + m * ldx, rows, ldx, w, static_cast<Y*>(y) + m * ldy, ldy, split, tiles});

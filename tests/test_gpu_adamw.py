@@ -46,7 +46,7 @@ def _host(t):
     return {k: (v.float() if v.dtype in (torch.bfloat16, torch.float16) else v).cpu().numpy().copy() for k, v in t.items()}
 
 
-def _check(before, t, i, step, bits, seed, scale=1.0, hyper=HYPER):
+def _check(before, t, i, step, bits, seed, scale=1.0, hyper=HYPER, words=None):
     lr, b1, b2, eps, decay = (hyper[k] for k in ("lr", "beta1", "beta2", "eps", "weight_decay"))
     old, new = before[i], _host(t)
     n = len(old["p"])
@@ -63,7 +63,7 @@ def _check(before, t, i, step, bits, seed, scale=1.0, hyper=HYPER):
         assert (np.abs(new["m"] - m) <= dm).all() and (np.abs(new["v"] - v) <= dv).all()
     else:
         m32, v32 = adamw.moments32(old["g"], m0.astype(np.float32), v0.astype(np.float32), b1, b2, scale)
-        words = adamw.random_words(n, step, seed + i)
+        words = adamw.random_words(n, step, seed + i) if words is None else words
         for k, x, w in (("m", m32, words & 0xFFFF), ("v", v32, words >> 16)):
             codes, scales = adamw.write(x, w, k)
             assert np.array_equal(new[k + "_scale"], scales)
@@ -175,6 +175,30 @@ def test_reading_every_state():
             want = adamw.read(codes, scales, k).astype(np.float32).astype(np.float64)
         used = (codes & 127) < 127 if k == "m" else codes < 248  # the others are never written
         assert np.array_equal(got[used], want[used], equal_nan=True)
+
+
+def test_a_tensor_of_more_than_2_to_the_32_elements():
+    """Element and block numbers and byte offsets past 32 bits; parts at both ends and around 2^32 against the oracle."""
+    n = 2 ** 32 + 1000
+    p, g = torch.full((n,), 0.5, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = (torch.full((n,), 0x38, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.full(((n + 31) // 32,), k, dtype=torch.uint8, device="cuda") for k in (117, 107))
+    gen, parts = torch.Generator("cuda").manual_seed(3), [(0, 96), (2 ** 31 - 32, 64), (2 ** 32 - 64, 128), (n - 40, 40)]
+    for at, k in parts:  # the last one begins within a block, whose other elements are as they were made
+        g[at:at + k] = torch.randn(k, generator=gen, device="cuda") * 1e-3
+    spans = [(at // 32 * 32, at + k) for at, k in parts]
+
+    def copies():
+        return [{k: x[a // 32:-(-b // 32)] if "scale" in k else x[a:b] for k, x in
+                 dict(p=p, g=g, m=m, v=v, m_scale=ms, v_scale=vs).items()} for a, b in spans]
+
+    before = [_host(t) for t in copies()]
+    plan = hp.AdamW([dict(p=p, g=g, m=m, v=v, m_scale=ms, v_scale=vs)], state_bits=8, seed=11)
+    plan.step(3, **HYPER)
+    torch.cuda.synchronize()
+    for (a, b), old, t in zip(spans, before, copies()):
+        words = adamw.random_words(b - a, 3, 11, first=a)
+        _check([old], t, 0, 3, 8, 11, words=words)
 
 
 @pytest.mark.parametrize("grad", GRADS, ids=str)

@@ -1,5 +1,7 @@
 """4-bit microscaled matrices on the GPU against the 64-bit oracle: codes and scales bit for bit,
 products within the rounding of their sums (and exactly where every sum is representable)."""
+from concurrent.futures import ThreadPoolExecutor
+
 import numpy as np
 import pytest
 import torch
@@ -79,6 +81,52 @@ def test_one_form_alone(form):
     hp.mx4_quantize(x.bfloat16(), *((None, q) if form else (q,)))
     x64 = x.bfloat16().double().cpu().numpy()
     _check(q, codes, scales, *mx4.quantize(x64.T if form else x64))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("rows,cols", [(67, 150), (1300, 150), (1027, 33)])
+def test_rows_alone(rows, cols, stochastic, dtype):
+    """Few rows, and so many that a wave takes eight."""
+    x = torch.from_numpy(_data(rows, cols, 3)).to("cuda", dtype)
+    q, codes, scales = _empty(rows, cols)
+    hp.mx4_quantize(x, q, rounding=int(stochastic), seed=6, epoch=2)
+    _check(q, codes, scales, *mx4.quantize(x.double().cpu().numpy(), stochastic, epoch=2, seed=6))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("rows,cols", [(1, 5000), (70, 200), (1300, 150), (33000, 40), (2100, 4200)])
+def test_forms_alone_and_together(rows, cols, stochastic, dtype):
+    """The forms do not depend on each other, nor on whether one workgroup makes both of a tile or two do."""
+    g = torch.Generator("cuda").manual_seed(rows)
+    x = torch.randn(rows, cols, generator=g, device="cuda").to(dtype)
+    how = dict(rounding=int(stochastic), seed=2, epoch=5)
+    (q, *a), (qt, *b), (both, *c), (both_t, *d) = _empty(rows, cols), _empty(cols, rows), _empty(rows, cols), _empty(cols, rows)
+    hp.mx4_quantize(x, q, **how)
+    hp.mx4_quantize(x, None, qt, **how)
+    hp.mx4_quantize(x, both, both_t, **how)
+    for one, two in ((a, c), (b, d)):
+        assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("rows,cols,ld", [(300, 1, 1), (257, 3, 3), (100, 7, 7), (1500, 2, 2), (129, 2, 5), (3, 9, 9)])
+def test_rows_shorter_than_a_load(rows, cols, ld, stochastic, dtype):
+    """Few columns: what one lane reads holds several rows, and the last rows end the memory."""
+    x = torch.from_numpy(_data(rows, cols, 8)).to("cuda", dtype)
+    flat = torch.full(((rows - 1) * ld + cols,), float("nan"), device="cuda", dtype=dtype)
+    held = flat.as_strided((rows, cols), (ld, 1))
+    held.copy_(x)
+    (q, codes, scales), (qt, codes_t, scales_t) = _empty(rows, cols), _empty(cols, rows)
+    hp.mx4_quantize(held, q, qt, rounding=int(stochastic), seed=4, epoch=7)
+    x64 = x.double().cpu().numpy()
+    _check(q, codes, scales, *mx4.quantize(x64, stochastic, epoch=7, seed=4))
+    _check(qt, codes_t, scales_t, *mx4.quantize(x64.T, stochastic, epoch=7, seed=4, purpose=7))
+    q, codes, scales = _empty(rows, cols)
+    hp.mx4_quantize(held, q, rounding=int(stochastic), seed=4, epoch=7)
+    _check(q, codes, scales, *mx4.quantize(x64, stochastic, epoch=7, seed=4))
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
@@ -343,6 +391,17 @@ def test_offsets_past_32_bits():
     assert ((out[:2] - want).abs() <= cols * 2.0 ** -23 * back.double().abs().sum(1)).all()
 
 
+def test_more_tiles_than_a_launch():
+    """2^24 + 3 tiles of 32 rows; powers of two are read back as they were."""
+    rows = 2 ** 29 + 77
+    c = torch.randint(0, 16, (rows, 1), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    x = torch.exp2((c & 7).to(torch.bfloat16) - 3) * (1 - 2 * (c >> 3).to(torch.bfloat16))
+    q, back = hp.mx4_empty(rows, 1), torch.full_like(x, float("nan"))
+    hp.mx4_quantize(x, q)
+    hp.mx4_dequantize(q, back)
+    assert torch.equal(back, x)
+
+
 def test_the_gradients_of_a_product():
     """L = sum(dY * (A B^T)) with every matrix representable along both axes: the gradients by products of the
     transposed forms are the formula's exactly, and a change of one entry changes L by the gradient's share."""
@@ -417,6 +476,36 @@ def test_another_stream_and_replayed_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(st[k], want[k]) for k in names), turn
+
+
+def test_calls_at_once_on_two_streams():
+    """Products of one size with a workspace each, and row products whose workgroups hold much and little of LDS."""
+    (a, _), (b, _), (c, _), (w, _) = (_random(r, 20_000, s) for r, s in ((100, 1), (200, 2), (100, 3), (4000, 4)))
+    x = torch.randn(16, 20_000, generator=torch.Generator("cuda").manual_seed(5), device="cuda")
+    short, _ = _random(4000, 300, 6)
+    n = hp.mx4_product_workspace(100, 200, 20_000)
+    assert n > 0
+
+    def calls(a, room, out, rows_out, stream):
+        for _ in range(20):
+            hp.mx4_product(a, b, out, workspace=room, stream=stream)
+            hp.mx4_row_product(x[:, :300], short, rows_out[0], stream=stream)
+            hp.mx4_row_product(x, w, rows_out[1], stream=stream)
+
+    def fresh():
+        return torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(100, 200, device="cuda"), torch.empty(2, 16, 4000, device="cuda")
+
+    want = [fresh(), fresh()]
+    for m, buffers in zip((a, c), want):
+        calls(m, *buffers, None)
+    got, streams = [fresh(), fresh()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    with ThreadPoolExecutor(2) as pool:
+        for done in [pool.submit(calls, m, *buffers, s.cuda_stream) for m, buffers, s in zip((a, c), got, streams)]:
+            done.result()
+    torch.cuda.synchronize()
+    for u, v in zip(want, got):
+        assert torch.equal(u[1], v[1]) and torch.equal(u[2], v[2])
 
 
 def test_a_workspace_that_is_too_small_is_left_alone():
