@@ -62,82 +62,124 @@ __device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
   return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
 }
 
-// ROWS rows of one operand for a tile: where a lane loads from.  In LDS codes lie row after row, and so do scales.
+// The codes of ROWS rows of one operand for a tile: where a lane loads from.  In LDS they lie row after row.
 template <int ROWS, int THREADS>
-struct Source {
-  static constexpr int kPieces = ROWS * 8 / THREADS, kWords = ROWS * 2 / THREADS;
-  static constexpr int kLoads = kPieces + kWords;  // per lane and stage
-  static_assert(kPieces * THREADS == ROWS * 8 && kWords * THREADS == ROWS * 2, "");
-  const uint8_t *codes, *scales;
-  uint32_t off[kPieces], word[kWords];
+struct Codes {
+  static constexpr int kLoads = ROWS * 8 / THREADS;  // per lane and stage
+  static_assert(kLoads * THREADS == ROWS * 8, "");
+  const uint8_t* base;
+  uint32_t off[kLoads];
 
   __device__ __forceinline__ void init(const MxView& m, int64_t row0, int64_t stage0) {
-    codes = scalar(m.codes + row0 * m.ldc + stage0 * kStage);
-    scales = scalar(m.scales + row0 * m.lds + stage0 * 8);
+    base = scalar(m.codes + row0 * m.ldc + stage0 * kStage);
     // rows past the end repeat the last one; 256 rows of less than 2^23 bytes are within 32 bits
     const uint32_t last = (uint32_t)min((int64_t)ROWS - 1, m.rows - 1 - row0);
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
+    for (int i = 0; i < kLoads; ++i) {
       const uint32_t p = i * THREADS + threadIdx.x, r = p / 8;
       off[i] = min(r, last) * (uint32_t)m.ldc + 16 * ((p ^ r / 2) & 7);
       asm volatile("" : "+v"(off[i]));  // one register: the compiler would keep the 64-bit multiply-add's two
     }
+  }
+  // load i of stage s to LDS address c.  half: the stage has one group only, which is read in place of the other.
+  __device__ __forceinline__ void fetch(int i, int64_t s, bool half, uint32_t c, uint32_t on) const {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), p = i * THREADS + threadIdx.x;
+    to_lds(scalar(base + s * kStage), off[i] - (half ? 16 * ((p ^ (p / 16)) & 4) : 0), c + i * THREADS * 16 + wave * 1024, on);
+  }
+};
+
+// The scales of both operands' rows, 16 bytes of a row at a time, two stages: a load takes about two cycles of the CU for each
+// line of memory that it touches, and the 8 bytes of a stage alone took 0.24 us beside the codes' 0.41 in
+// tiles of 128.  (Four stages at a time are no faster: their words meet on fewer banks, or more loads are left out, which
+// take their time too.)  In LDS they lie row after row, a's first.
+template <int BM, int BN, int THREADS>
+struct Scales {
+  static constexpr int kLoads = (BM + BN) / THREADS, kPair = (BM + BN) * 16;
+  static_assert(kLoads * THREADS == BM + BN && BM % 64 == 0, "a wave's load is of one operand");
+  const uint8_t *a, *b;
+  uint32_t off[kLoads], begin, last;  // begin: of the first stage in a row; last: where the last 16 bytes of a row begin
+
+  __device__ static __forceinline__ uint32_t row_at(const MxView& ma, const MxView& mb, int64_t m0, int64_t n0, int row) {
+    return row < BM ? (uint32_t)min((int64_t)row, ma.rows - 1 - m0) * (uint32_t)ma.lds
+                    : (uint32_t)min((int64_t)row - BM, mb.rows - 1 - n0) * (uint32_t)mb.lds;
+  }
+  __device__ __forceinline__ void init(const MxView& ma, const MxView& mb, int64_t m0, int64_t n0, int64_t groups, int first) {
+    a = scalar(ma.scales + m0 * ma.lds);
+    b = scalar(mb.scales + n0 * mb.lds);
+    begin = 8 * first;
+    last = groups < 4 ? ~0u / 2 : (uint32_t)(4 * groups - 16);
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      const uint32_t w = i * THREADS + threadIdx.x;
-      word[i] = min(w / 2, last) * (uint32_t)m.lds + 4 * (w % 2);
-      asm volatile("" : "+v"(word[i]));
+    for (int i = 0; i < kLoads; ++i) {
+      off[i] = row_at(ma, mb, m0, n0, i * THREADS + threadIdx.x);
+      asm volatile("" : "+v"(off[i]));
     }
   }
-  // load i of stage s to the buffers at LDS addresses c (codes) and k (scales).  half: the stage has one group only,
-  // which is read in place of the other.
-  __device__ __forceinline__ void fetch(int i, int64_t s, bool half, uint32_t c, uint32_t k, uint32_t on) const {
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (i < kPieces) {
-      const uint32_t p = i * THREADS + threadIdx.x;
-      to_lds(scalar(codes + s * kStage), off[i] - (half ? 16 * ((p ^ (p / 16)) & 4) : 0), c + i * THREADS * 16 + wave * 1024, on);
-    } else {
-      i -= kPieces;
-      const uint32_t w = i * THREADS + threadIdx.x;
-      word_to_lds(scalar(scales + s * 8), word[i] - (half ? 4 * (w % 2) : 0), k + i * THREADS * 4 + wave * 256, on);
+  // Load i of the stages s and s + 1 (s even) to LDS address k.  What would reach past the row is read from its last 16 bytes
+  // instead: see moved().
+  __device__ __forceinline__ void fetch(int i, int s, uint32_t k, uint32_t on) const {
+    const uint32_t p = i * THREADS + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 64;
+    to_lds(scalar(p < BM ? a : b), off[i] + min(begin + 8 * s, last), k + p * 16, on);
+  }
+  // The first two stages of rows with fewer than four groups, which have no 16 bytes: word by word, the last one in place
+  // of those that are not there.
+  __device__ __forceinline__ void fetch_words(const MxView& ma, const MxView& mb, int64_t m0, int64_t n0, int64_t groups, uint32_t k) const {
+#pragma unroll 1
+    for (int i = 0; i < 4 * kLoads; ++i) {
+      const uint32_t p = i * THREADS + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 64;
+      const uint32_t word = min(4 * (threadIdx.x % 4), (uint32_t)(4 * groups - 4));
+      word_to_lds(scalar(p < 4 * BM ? a : b), row_at(ma, mb, m0, n0, (i * THREADS + threadIdx.x) / 4) + word, k + p * 4, ~0u);
     }
+  }
+  // how far stage s lies behind its place, since its 16 bytes were read from before
+  __device__ __forceinline__ uint32_t moved(int s) const {
+    const uint32_t at = begin + 8 * (s & ~1);
+    return at > last ? at - last : 0;
   }
 };
 
 // Tiles of WM FM x WN FN fragments, one wave FM x FN of them.  A stage is four steps (block j of each group) of FM x FN
 // products.  A step's fragments are read during the step before; the barrier that a stage has arrived for
 // stands one step before its first product, when all of the stage before has been read, so that the
-// matrix cores do not wait for it.  D buffers: D - 1 stages are on their way or in use.
+// matrix cores do not wait for it.  D buffers: D - 1 stages are on their way or in use.  Scales come in pairs of
+// stages, each asked for when the pair before it begins, into two buffers of their own.
 template <typename T, int WM, int WN, int FM, int FN, int D>
 __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
   constexpr int kThreads = WM * WN * 64, BM = WM * FM * 32, BN = WN * FN * 32;
-  constexpr int kCodes = (BM + BN) * kStage, kBuffer = kCodes + (BM + BN) * 8;
-  __shared__ __align__(16) uint8_t lds[D * kBuffer];
+  constexpr int kBuffer = (BM + BN) * kStage;
+  using S = Scales<BM, BN, kThreads>;
+  static_assert(D <= 3, "a pair of scales has arrived D - 1 stages after it was asked for, and is read after two");
+  __shared__ __align__(16) uint8_t lds[2 * S::kPair + D * kBuffer];
 
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 32, h = lane / 32;
   const int wm = wave / WN, wn = wave % WN;
-  // workgroups go to the XCDs in turn: each XCD takes a run of tiles, in bands of eight tile rows
-  const int total = a.tiles_m * a.tiles_n, x = blockIdx.x % 8, i = blockIdx.x / 8;
-  const int tile = x * (total / 8) + min(x, total % 8) + i, cut = blockIdx.y;
+  // workgroups go to the XCDs in turn: each XCD takes a run of the cuts' tiles, in bands of eight tile rows, so that it
+  // reads its cuts of K only
+  const int tiles = a.tiles_m * a.tiles_n, total = tiles * a.cuts, at = blockIdx.y * tiles + blockIdx.x, x = at % 8;
+  const int item = x * (total / 8) + min(x, total % 8) + at / 8, cut = item / tiles, tile = item % tiles;
   const int band = tile / (8 * a.tiles_n), rest = tile % (8 * a.tiles_n), height = min(8, a.tiles_m - 8 * band);
   const int64_t m0 = (int64_t)(8 * band + rest % height) * BM, n0 = (int64_t)(rest / height) * BN;
 
-  Source<BM, kThreads> sa;
-  Source<BN, kThreads> sb;
+  Codes<BM, kThreads> ca;
+  Codes<BN, kThreads> cb;
+  S sc;
   const int64_t groups = mx_groups(a.a.cols), all = (groups + 1) / 2;
   const int first = (int)(all * cut / a.cuts), stages = (int)(all * (cut + 1) / a.cuts) - first;
   const bool odd = (groups & 1) && cut == a.cuts - 1;  // the last stage has one group
-  sa.init(a.a, m0, first);
-  sb.init(a.b, n0, first);
+  ca.init(a.a, m0, first);
+  cb.init(a.b, n0, first);
+  sc.init(a.a, a.b, m0, n0, groups, first);
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LPtr)lds;
-  constexpr int kLoads = sa.kLoads + sb.kLoads;
-  const auto fetch = [&](int i, int s, int buffer) {  // load i of stage s
-    const uint32_t at = lds0 + buffer * kBuffer;
+  // every stage asks for as many, left out or not, so that they can be counted
+  constexpr int kLoads = ca.kLoads + cb.kLoads + sc.kLoads;
+  const auto fetch = [&](int i, int s, int buffer, int pair) {  // load i: codes of stage s; scales of stages pair, pair + 1
+    const uint32_t at = lds0 + 2 * S::kPair + buffer * kBuffer;
     const bool half = odd && s == stages - 1;
     const uint32_t on = __builtin_amdgcn_readfirstlane(s < stages ? ~0u : 0u);
-    if (i < sa.kLoads) sa.fetch(i, s, half, at, at + kCodes, on);
-    else if (i < kLoads) sb.fetch(i - sa.kLoads, s, half, at + BM * kStage, at + kCodes + BM * 8, on);
+    if (i < ca.kLoads) ca.fetch(i, s, half, at, on);
+    else if (i < ca.kLoads + cb.kLoads) cb.fetch(i - ca.kLoads, s, half, at + BM * kStage, on);
+    else if (i < kLoads)
+      sc.fetch(i - ca.kLoads - cb.kLoads, pair, lds0 + pair / 2 % 2 * S::kPair, __builtin_amdgcn_readfirstlane(pair % 2 == 0 && pair < stages ? ~0u : 0u));
   };
 
   v16f32 acc[FM][FN] = {};
@@ -151,17 +193,18 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
     for (int n = 0; n < FN; ++n) acc[m][n] = mfma4<j>(fy[j % 2][n], fx[j % 2][m], acc[m][n], sy[n], sx[m]);
   };
 
+  if (stages && groups < 4) sc.fetch_words(a.a, a.b, m0, n0, groups, lds0);
 #pragma unroll
   for (int s = 0; s < D - 1; ++s)
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) fetch(i, s, s);
+    for (int i = 0; i < kLoads; ++i) fetch(i, s, s, s == 0 && groups >= 4 ? 0 : 1);
   int buffer = 0, free = D - 1;  // of this stage; of the next one that is asked for
   for (int s = 0; s < stages; ++s) {
     // this stage has arrived (the loads of those behind it may be under way), and every wave has read the one before
     static_assert((D - 2) * kLoads < 64, "");
     if (D > 2 && s + D - 2 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * kLoads) : "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const uint8_t* codes = lds + buffer * kBuffer;
+    const uint8_t* codes = lds + 2 * S::kPair + buffer * kBuffer;
     // Row m of the products of a step, with a part of the next step's reads and of the next stage's loads before it.
     // The order is held: the compiler would put the reads behind the products, where they are waited for.
     const auto part = [&](auto step, int j, int m) {  // j: the step that is read
@@ -172,17 +215,17 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
       fx[j % 2][m] = *reinterpret_cast<const uint4*>(codes + ((wm * FM + m) * 32 + r) * kStage + piece);
       constexpr int kPer = (kLoads + 3 * FM - 1) / (3 * FM);  // all in the first three steps
 #pragma unroll
-      for (int n = 0; n < kPer; ++n) fetch((j * FM + m) * kPer + n, s + D - 1, free);
+      for (int n = 0; n < kPer; ++n) fetch((j * FM + m) * kPer + n, s + D - 1, free, s + 2);
       __builtin_amdgcn_sched_barrier(0);
       products(step, m);
       __builtin_amdgcn_sched_barrier(0);
     };
     uint32_t nx[FM], ny[FN];
-    const uint32_t* scales = reinterpret_cast<const uint32_t*>(codes + kCodes) + h;
+    const uint8_t* scales = lds + s / 2 % 2 * S::kPair + 8 * (s % 2) + 4 * h + sc.moved(s);
 #pragma unroll
-    for (int m = 0; m < FM; ++m) nx[m] = scales[2 * ((wm * FM + m) * 32 + r)];
+    for (int m = 0; m < FM; ++m) nx[m] = *reinterpret_cast<const uint32_t*>(scales + 16 * ((wm * FM + m) * 32 + r));
 #pragma unroll
-    for (int n = 0; n < FN; ++n) ny[n] = scales[2 * (BM + (wn * FN + n) * 32 + r)];
+    for (int n = 0; n < FN; ++n) ny[n] = *reinterpret_cast<const uint32_t*>(scales + 16 * (BM + (wn * FN + n) * 32 + r));
 #pragma unroll
     for (int m = 0; m < FM; ++m) part(std::integral_constant<int, 3>{}, 0, m);
     // The group that an odd row's last stage lacks gets scales of 0 on both sides, 2^-254 together: what was read in
@@ -273,11 +316,12 @@ namespace {
 
 // How a product is made: the edge of its tiles (256, 128, 64: one, two, three workgroups to a CU) and the parts that K is
 // cut in.  Small tiles fill the CUs where there are few, at the price of more reads; parts cost a pass over
-// them.  The choice is the least of an estimate in microseconds fitted to timings on this GPU: a stage takes 2.0
-// with 256-tiles on every CU (1.2 with a few: the power limit), 0.78 and 1.5 with one and two 128-tiles
-// on a CU, 0.42 to 0.93 with one to three 64-tiles; beginning and ending a tile 12, 4 and 2.4.  On both sides of its
-// borders (measured, us): 4096 x 4096 x 2048 29 / 34 / 53 with 256 / 128 / 64, 4096 x 2048 x 4096 34 / 29 / 48,
-// 300 x 4096 x 4096 27 / 14 / 13; 1000 x 784 x 60000 with 128 in 1, 2, 4, 8, 16 parts 176, 100, 62, 69, 77.
+// them.  The choice is the least of an estimate in microseconds fitted to timings of 21 sizes on this GPU (its choices take
+// 1 % longer than the best there, the worst 10 %): a stage takes 1.9 with 256-tiles on every CU (1.0 with a few: the
+// power limit), 0.77 and 1.27 with one and two 128-tiles on a CU, 0.42 to 0.8 with one to three 64-tiles; beginning and
+// ending a tile 10.5, 4 and 3.4.  On both sides of its borders (measured, us): 4096 x 4096 x 2048 28 / 29 / 44 with
+// 256 / 128 / 64, 4096 x 2048 x 4096 31 / 26 / 42, 300 x 4096 x 4096 27 / 13.3 / 13.0; 1000 x 784 x 60000 with 128 in
+// 1, 2, 4, 8, 16 parts 152, 82, 50, 49, 57.
 struct Plan {
   int tile, cuts;
 };
@@ -286,20 +330,20 @@ Plan plan(int64_t M, int64_t N, int64_t K, int cus) {
   const int64_t stages = (mx_groups(K) + 1) / 2;
   const auto stage_us = [&](int tile, double per_cu) {  // workgroups per CU
     const int n = (int)std::ceil(per_cu);
-    if (tile == 256) return 1.2 + 0.8 * (per_cu < 1 ? per_cu : 1);
-    if (tile == 128) return n == 1 ? 0.78 : 1.5;
-    return n == 1 ? 0.42 : n == 2 ? 0.7 : 0.93;
+    if (tile == 256) return 1.0 + 0.9 * (per_cu < 1 ? per_cu : 1);
+    if (tile == 128) return n == 1 ? 0.77 : 1.27;
+    return n == 1 ? 0.42 : n == 2 ? 0.61 : 0.8;
   };
   Plan best{128, 1};
   double least = 1e300;
   for (int tile = 256, most = 1; tile >= 64; tile /= 2, ++most)
     for (int cuts = 1; cuts == 1 || (cuts <= 16 && stages / cuts >= 4); cuts *= 2) {
       const double blocks = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * cuts / cus;  // per CU
-      const double ends = tile == 256 ? 12 : tile == 128 ? 4 : 2.4, full = std::floor(blocks / most), rest = blocks - full * most;
+      const double ends = tile == 256 ? 10.5 : tile == 128 ? 4 : 3.4, full = std::floor(blocks / most), rest = blocks - full * most;
       const double length = (double)((stages + cuts - 1) / cuts);
       double us = full * (length * stage_us(tile, most) + ends);
       if (rest > 0) us += length * stage_us(tile, rest) + ends;
-      if (cuts > 1) us += 3.5 + (double)cuts * M * N * 8 / 6e6;
+      if (cuts > 1) us += 4.4 + (double)cuts * M * N * 8 / 8.5e6;
       if (us < least) least = us, best = Plan{tile, cuts};
     }
   return best;
@@ -326,7 +370,7 @@ int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, 
     const dim3 grid((unsigned)(tm * tn), (unsigned)p.cuts);
     if (p.tile == 256) hipLaunchKernelGGL((product_tiles<T, 2, 4, 4, 2, 2>), grid, dim3(512), 0, s, args);
     // 128: two buffers let two workgroups share a CU; where each has one to itself, a third hides the loads' latency
-    // (1000 x 784 x 60000 in four parts 74 and 62 us, 4096 x 4096 x 4096 60 and 74)
+    // (1000 x 784 x 60000 in four parts 63 and 50 us, 4096 x 4096 x 4096 49 and 60)
     else if (p.tile == 128 && tm * tn * p.cuts > cus) hipLaunchKernelGGL((product_tiles<T, 2, 2, 2, 2, 2>), grid, dim3(256), 0, s, args);
     else if (p.tile == 128) hipLaunchKernelGGL((product_tiles<T, 2, 2, 2, 2, 3>), grid, dim3(256), 0, s, args);
     else hipLaunchKernelGGL((product_tiles<T, 1, 2, 2, 1, 3>), grid, dim3(128), 0, s, args);
