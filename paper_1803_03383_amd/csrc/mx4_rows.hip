@@ -104,6 +104,27 @@ __global__ __launch_bounds__(64 * kWaves) void row_product(RowArgs a) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) put(m + u, v[u]);
       }
+    // The wave in which the rows end: lanes beyond read the rows' last 16 bytes and move them to their place, with zeros
+    // behind, several rows under way here too (value by value, row after row, 13 rows of 5000 took 1.4 us longer).
+    else if (a.w.cols >= kV) {
+      const int bytes = (int)(kV - min(max(left, (int64_t)0), (int64_t)kV)) * (int)sizeof(X);
+      const X* from = static_cast<const X*>(a.x) + min(kV * (int64_t)p, a.w.cols - kV);
+      for (; m + kAhead <= rows; m += kAhead) {
+        uint4 v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) v[u] = mx_load16(from + (m + u) * a.ldx, kV);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          uint4 w = v[u];
+          if (sizeof(X) == 2 && bytes & 2)
+            w = uint4{__builtin_amdgcn_alignbyte(w.y, w.x, 2), __builtin_amdgcn_alignbyte(w.z, w.y, 2), __builtin_amdgcn_alignbyte(w.w, w.z, 2), w.w >> 16};
+          if (bytes & 4) w = uint4{w.y, w.z, w.w, 0};
+          if (bytes & 8) w = uint4{w.z, w.w, 0, 0};
+          if (bytes & 16) w = uint4{};
+          put(m + u, w);
+        }
+      }
+    }
 #pragma unroll 1
     for (; m < rows; ++m) put(m, mx_load16(x + m * a.ldx, left));
   }

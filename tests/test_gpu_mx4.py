@@ -346,6 +346,24 @@ def test_row_product_of_rows_at_any_offset(offset):
     assert (np.abs(out.double().cpu().numpy() - want) <= _bound(xv, wv, torch.float32, want)).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_row_product_of_rows_that_end_anywhere(dtype):
+    """Powers of two on either side of w's rows of unit vectors: y holds the last columns of x themselves."""
+    for K in [*range(1, 20), *range(505, 530), 1537, 4093]:
+        n = min(K, 40)
+        e = torch.zeros(n, K, device="cuda")
+        e[torch.arange(n), K - n + torch.arange(n)] = 1
+        w = hp.mx4_empty(n, K)
+        hp.mx4_quantize(e, w)
+        g = torch.Generator("cuda").manual_seed(K)
+        flat = torch.full((9 * (K + 3),), float("nan"), device="cuda", dtype=dtype)[:8 * (K + 3) + K]
+        x = flat.as_strided((9, K), (K + 3, 1))
+        x.copy_(torch.exp2(torch.randint(0, 3, (9, K), generator=g, device="cuda").float()))
+        out = torch.empty(9, n, device="cuda")
+        hp.mx4_row_product(x, w, out)
+        assert torch.equal(out, x[:, K - n:].float()), K
+
+
 def test_row_product_with_rows_that_are_not_finite():
     w, _ = _random(40, 500, 10)
     x = torch.ones(6, 500, device="cuda")
