@@ -359,13 +359,13 @@ def _matrix(t, what, rows=None, cols=None):
 
 def _same_device(t, *others):
     """The index of the GPU that all tensors are on."""
-    dev = t.device
+    dev = t.get_device()
     for o in others:
-        if o is not None and o.device != dev:
-            raise ValueError(f"tensors on {dev} and {o.device}")
-    if dev.type != "cuda":
-        raise ValueError(f"GPU tensors expected, not {dev}")
-    return dev.index
+        if o is not None and o.get_device() != dev:
+            raise ValueError(f"tensors on {t.device} and {o.device}")
+    if dev < 0:
+        raise ValueError(f"GPU tensors expected, not {t.device}")
+    return dev
 
 
 def _run(name, dev, stream, *args):
