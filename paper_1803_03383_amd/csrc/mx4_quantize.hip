@@ -29,25 +29,20 @@ __device__ __forceinline__ v2u16 odd_pair(uint32_t w0, uint32_t w1, int e) {
   return __builtin_bit_cast(v2u16, r << 1 | 0x00010001u);
 }
 
-// Codes of two values.  z = floor(1024 t) of t = |x| / scale, at most 6144, fits 16 bits; the step is 512 2^k of it, and
-// the fraction's comparison with (511 - 2 r) / 512 is the carry of (z >> k) + 2 r + 1 past 512.
-__device__ __forceinline__ uint32_t codes_pair(float a, float b, int up, v2u16 odd) {
-  const v2u16 z{(unsigned short)(uint32_t)ldexpf(__builtin_fabsf(a), up), (unsigned short)(uint32_t)ldexpf(__builtin_fabsf(b), up)};
-  const v2u16 k = __builtin_elementwise_min(z >> v2u16{11, 11}, v2u16{2, 2});
-  const v2u16 c = (((z >> k) + odd) >> v2u16{9, 9}) + k + k;
-  // the signs, from the top bytes
-  const uint32_t top = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x0C070C03u);
-  return __builtin_bit_cast(uint32_t, c) | (top >> 4 & 0x00080008u);
-}
-
-// codes of N = 4 or 8 values in order, from the random bytes of w0 (the first four) and w1
+// Codes of N = 4 or 8 values in order, from the random bytes of w0 (the first four) and w1.  The bits of 2^-14 t in fp16, t =
+// |x| / scale <= 6 and cut towards zero, are 512 times the code of the grid's value below t and the fraction in 512ths
+// of the step (below 1 it is subnormal, which is the grid's step of 1/2), so that the fraction's comparison with
+// (511 - 2 r) / 512 is the carry of adding 2 r + 1: 5 instructions a value.
 template <int N>
 __device__ __forceinline__ uint32_t codes_random(const float* v, uint32_t s, uint32_t w0, uint32_t w1) {
-  const int up = 137 - (int)s;
+  const int down = 113 - (int)s;
   uint32_t c = 0;
 #pragma unroll
-  for (int e = 0; e < N / 2; ++e)  // values e and e + N / 2 end up in the low and the high half
-    c |= codes_pair(v[e], v[e + N / 2], up, N == 8 ? odd_pair(w0, w1, e) : odd_pair(w0, w0 >> 16, e)) << (4 * e);
+  for (int e = 0; e < N / 2; ++e) {  // values e and e + N / 2 end up in the low and the high half
+    const v2u16 t = __builtin_bit_cast(v2u16, __builtin_amdgcn_cvt_pkrtz(ldexpf(v[e], down), ldexpf(v[e + N / 2], down)));
+    const uint32_t p = __builtin_bit_cast(uint32_t, (v2u16)(t + (N == 8 ? odd_pair(w0, w1, e) : odd_pair(w0, w0 >> 16, e))));
+    c |= ((e < 3 ? p >> (9 - 4 * e) : p << 3) & 0x00070007u << 4 * e) | (p >> (12 - 4 * e) & 0x00080008u << 4 * e);
+  }
   if (N == 4) c = (c | c >> 8) & 0xFFFFu;
   return s == 255u ? 0u : c;
 }
