@@ -1,7 +1,7 @@
 // Products of MX4 matrices on the matrix cores: c = a b^T (+ c).
 //
 // A workgroup makes a tile of c.  Stages of 256 values of K (128 bytes of codes and 8 scales a row) of both
-// operands go to LDS by global_load_lds, in two to four buffers; a wave reads fragments of 32 rows and multiplies
+// operands go to LDS by global_load_lds, in two or three buffers; a wave reads fragments of 32 rows and multiplies
 // them with v_mfma_scale_f32_32x32x64_f8f6f4 in 4 bits (the 16x16x128 form sustains 5.1 - 5.9
 // PFLOP/s on random codes, this one 6.8, where the power limit holds it).  The order of K within a stage
 // is free as long as both operands have the same: lane half h takes the four blocks of group h of a row,
