@@ -379,7 +379,7 @@ int halp_debug_step_latency(int32_t waves, int64_t steps, int32_t blocks, uint32
 
 typedef struct {
   void* codes;    /* DEVICE [rows][ldc], 16-byte aligned                                        */
-  int64_t ldc;    /* bytes from row to row, a multiple of 16 (multiples of 128 are read fastest),
+  int64_t ldc;    /* bytes from row to row, a multiple of 16 (128: read a little faster),
                      >= 64 ceil(cols / 128), < 2^23                                             */
   uint8_t* scales; /* DEVICE [rows][lds], 4-byte aligned                                        */
   int64_t lds;    /* bytes from row to row, a multiple of 4, >= 4 ceil(cols / 128), < 2^23     */
