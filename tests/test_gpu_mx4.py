@@ -236,6 +236,33 @@ def test_large_products_are_exact(M, N, K):
     assert torch.equal(c, want.float() + 1)
 
 
+@pytest.mark.parametrize("M,N", [(100, 90), (2000, 1900), (2100, 2300), (4200, 4000)])
+def test_products_of_every_number_of_groups(M, N):
+    """Scales that differ from block to block, rows that end at any place of the pieces in which they are read, parts that
+    begin at odd ones.  Values are multiples of 1/4 of at most 12: sums of K products, in sixteenths at most 2304 K, are
+    below 2^24 and exact in any order."""
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6], device="cuda")
+    g = torch.Generator("cuda").manual_seed(M)
+
+    def make(rows, K):
+        blocks = -(-K // 32)
+        x = grid[torch.randint(0, 8, (rows, K), device="cuda", generator=g)] * torch.randint(-1, 2, (rows, K), device="cuda", generator=g)
+        x *= torch.exp2(torch.randint(-1, 2, (rows, blocks), device="cuda", generator=g).float()).repeat_interleave(32, 1)[:, :K]
+        q = hp.mx4_empty(rows, K)
+        hp.mx4_quantize(x, q)
+        return x.double(), q
+
+    for groups in [*range(1, 19), 40, 41, 51, 56]:
+        K = 128 * groups - 30
+        assert 2304 * K < 2 ** 24
+        (a, qa), (b, qb) = make(M, K), make(N, K)
+        want = (a @ b.t()).float()
+        for cut in (False, True):
+            out = torch.full((M, N), float("nan"), device="cuda")
+            _product(qa, qb, out, cut=cut)
+            assert torch.equal(out, want), (K, cut)
+
+
 def _bound(av, bv, dtype, want):
     """K roundings of a sum of K products, each at most a step of the sum of magnitudes, and the type's rounding."""
     sums = av.shape[1] * 2.0 ** -23 * np.abs(av).dot(np.abs(bv).T)
