@@ -1,8 +1,8 @@
 // Matrices into MX4, along their rows and along their columns, and back.
 //
 // Bound by memory: x is read once for both forms.  A wave holds a tile of R rows and 1 KB of each in registers, 16
-// bytes of a row per lane.  A block of a row then lies in four (16-bit types) or eight (fp32) adjacent lanes,
-// a block of a column in one lane (R = 32), so that no values move between waves; four waves take the four blocks of
+// bytes of a row per lane (eight where tiles are few).  A block of a row then lies in four or eight adjacent
+// lanes, a block of a column in one lane (R = 32), so that no values move between waves; four waves take the four blocks of
 // a stored group of the transposed form, and their codes meet in LDS to leave 64 bytes at a time.
 #include <utility>
 
@@ -47,75 +47,118 @@ __device__ __forceinline__ uint32_t codes_random(const float* v, uint32_t s, uin
   return s == 255u ? 0u : c;
 }
 
-// value e of a lane's 16 bytes
-template <typename T>
-__device__ __forceinline__ float value_at(uint4 v, int e) {
-  const uint32_t w = reinterpret_cast<const uint32_t*>(&v)[e * (int)sizeof(T) / 4];
+// V values of a lane as words
+template <typename T, int V>
+struct Piece {
+  static constexpr int kWords = V * sizeof(T) / 4;
+  uint32_t w[kWords];
+};
+
+// value e of a lane's
+template <typename T, int V>
+__device__ __forceinline__ float value_at(const Piece<T, V>& v, int e) {
+  const uint32_t w = v.w[e * (int)sizeof(T) / 4];
   if constexpr (std::is_same_v<T, float>) return __builtin_bit_cast(float, w);
   else if constexpr (std::is_same_v<T, __bf16>) return __builtin_bit_cast(float, e % 2 ? w & 0xFFFF0000u : w << 16);
   else return (float)__builtin_bit_cast(_Float16, (uint16_t)(e % 2 ? w >> 16 : w));
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t row_codes_random(uint4 v, uint32_t s, uint32_t w0, uint32_t w1) {
-  constexpr int kV = 16 / sizeof(T);
-  float f[kV];
+// the same as mx_max16 and mx_codes16 take it: zeros behind
+template <typename T, int V>
+__device__ __forceinline__ uint4 whole(const Piece<T, V>& v) {
+  if constexpr (Piece<T, V>::kWords == 4) return uint4{v.w[0], v.w[1], v.w[2], v.w[3]};
+  else return uint4{v.w[0], v.w[1], 0, 0};
+}
+
+template <typename T, int V>
+__device__ __forceinline__ uint32_t row_codes(const Piece<T, V>& v, uint32_t s) {
+  if constexpr (Piece<T, V>::kWords == 4) {
+    return mx_codes16<T>(whole(v), s);
+  } else {
+    const float scale = __builtin_bit_cast(float, s << 23);
+    const uint32_t c = mx_codes2<T, 1>(mx_codes2<T, 0>(0, v.w[0], 0, scale), v.w[1], 0, scale);
+    return s == 255u ? 0u : c;
+  }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ uint32_t row_codes_random(const Piece<T, V>& v, uint32_t s, uint32_t w0, uint32_t w1) {
+  float f[V];
 #pragma unroll
-  for (int e = 0; e < kV; ++e) f[e] = value_at<T>(v, e);
-  return codes_random<kV>(f, s, w0, w1);
+  for (int e = 0; e < V; ++e) f[e] = value_at(v, e);
+  return codes_random<V>(f, s, w0, w1);
 }
 
 // ---- a wave's tile -------------------------------------------------------------------------------
 
-template <typename T, int R>
+template <typename T, int R, int V>
 struct Tile {
-  static constexpr int kV = 16 / sizeof(T);
-  uint4 v[R];
+  static constexpr int kV = V, kWords = Piece<T, V>::kWords;
+  Piece<T, V> v[R];
 
-  // rows row0 .. and columns col .. col + kV - 1 of x, zeros outside.  A lane's 16 bytes may reach past the last
-  // column, into what lies between the rows or into the next one, and are masked; rows so near the end that they would
-  // reach past the last element are read value by value.
+  // rows row0 .. and columns col .. col + kV - 1 of x, zeros outside.  All loads are made, those of rows and columns
+  // outside from others, so that nothing stands between them.  A lane's piece may reach past the last
+  // column, into what lies between the rows or into the next one, and is masked; rows so near the end that such a piece
+  // would reach past the last element are read value by value.
   __device__ __forceinline__ void load(const QuantArgs& a, int64_t row0, int64_t col) {
-    const T* x = static_cast<const T*>(a.x) + row0 * a.ldx + col;
     const int64_t left = a.cols - col;  // of this lane's columns
-    const int rows = (int)min((int64_t)R, a.rows - row0);
-    const bool some = left > 0, ragged = __any(some && left < kV);
+    const bool ragged = __any(left < kV);
     const int64_t near = ragged ? a.rows - 1 - (kV - 2) / a.ldx : a.rows;  // the first such row
-    const int wide = (int)min((int64_t)rows, near - row0);
-    struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[4]; };
+    typedef uint32_t __attribute__((ext_vector_type(kWords))) Words;
+    typedef Words __attribute__((aligned(sizeof(T)))) Loose;
+    Words w[R] = {};
+    if (near > 0) {
+      const T* x = static_cast<const T*>(a.x) + (left > 0 ? col : 0) + min(row0, near - 1) * a.ldx;
+      const int more = __builtin_amdgcn_readfirstlane((int)min((int64_t)R, near - 1 - row0));  // rows after the first
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      v[i] = uint4{};
-      if (i < wide && some) {
-        const Loose l = *reinterpret_cast<const Loose*>(x + i * a.ldx);
-        v[i] = uint4{l.w[0], l.w[1], l.w[2], l.w[3]};
+      for (int i = 0; i < R; ++i) {
+        w[i] = *reinterpret_cast<const Loose*>(x);
+        x += i < more ? a.ldx : 0;
       }
     }
-    if (!ragged) return;
-    uint32_t mask[4];
+    const int rows = (int)max(min((int64_t)R, a.rows - row0), (int64_t)0);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      constexpr int kPer = kV / 4;  // values of a word
-      mask[k] = left >= (k + 1) * kPer ? ~0u : left > k * kPer ? 0xFFFFu : 0u;
-    }
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int i = 0; i < R; ++i) v[i] = uint4{v[i].x & mask[0], v[i].y & mask[1], v[i].z & mask[2], v[i].w & mask[3]};
-#pragma unroll 1
-    for (int64_t row = max(row0, near); row < row0 + rows; ++row) {
-      const uint4 u = mx_load16(x + (row - row0) * a.ldx, left);
+      for (int k = 0; k < kWords; ++k) v[i].w[k] = w[i][k];
+    if (rows < R) {
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        if (i == (int)(row - row0)) v[i] = u;
+        if (i >= rows) v[i] = Piece<T, V>{};
+    }
+    if (!ragged) return;
+    constexpr int kPer = kV / kWords;  // values of a word
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+      const uint32_t mask = left >= (k + 1) * kPer ? ~0u : left > k * kPer ? 0xFFFFu : 0u;
+#pragma unroll
+      for (int i = 0; i < R; ++i) v[i].w[k] &= mask;
+    }
+#pragma unroll 1
+    for (int64_t row = max(row0, near); row < row0 + rows; ++row) {
+      const T* from = static_cast<const T*>(a.x) + row * a.ldx + col;
+      uint32_t u[kWords] = {};
+#pragma unroll
+      for (int e = 0; e < kV; ++e)
+        if (e < left) {
+          if constexpr (sizeof(T) == 4) u[e] = __builtin_bit_cast(uint32_t, from[e]);
+          else u[e / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, from[e]) << (16 * (e % 2));
+        }
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int k = 0; k < kWords; ++k)
+          if (i == (int)(row - row0)) v[i].w[k] = u[k];
     }
   }
 };
 
-// Random words of this lane's values of row i of x: w0, w1 (16-bit types) or w0 (fp32) of the block of 16 columns that two
+// Random words of this lane's V values of row i of x: w0, w1 (eight) or w0 (four) of the block of 16 columns that two
 // or four adjacent lanes share.  Each of them makes the block of another row, and they exchange words: rows are taken
 // two or four at a time.
-template <typename T>
+template <int V>
 struct RowRandom {
-  static constexpr int kRows = sizeof(T) == 4 ? 4 : 2;  // rows at a time, and lanes that share a block
+  static constexpr int kRows = 16 / V;  // rows at a time, and lanes that share a block
   uint32_t w[kRows][2];
 
   __device__ __forceinline__ void make(const QuantArgs& a, int64_t row0, int64_t col) {
@@ -147,9 +190,9 @@ __device__ __forceinline__ void for_each_index(F&& f, std::integer_sequence<int,
   (f(std::integral_constant<int, I>{}), ...);
 }
 
-template <typename T, bool ROWS, bool COLS, bool RANDOM, int R>
+template <typename T, bool ROWS, bool COLS, bool RANDOM, int R, int V>
 __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
-  constexpr int kV = 16 / sizeof(T), kLanes = kMxBlock / kV;
+  constexpr int kV = V, kLanes = kMxBlock / kV;
   static_assert(!COLS || R == kMxBlock, "");
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   // The column blocks of the four waves meet here: blocks by value, lane and wave, the wave's place permuted so that lanes
@@ -161,25 +204,28 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
   const int forms = gridDim.y == 1 ? 3 : 1 << blockIdx.y;  // of a tile, by this workgroup
   for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
     const int64_t row0 = (t / a.across * 4 + wave) * R, col = (t % a.across * 64 + lane) * kV;
-    Tile<T, R> x;
+    Tile<T, R, V> x;
     x.load(a, row0, col);
     if (ROWS && forms & 1) {
       const bool stored = col < mx_groups(a.cols) * kMxGroup;
       uint8_t *codes = a.q.codes + row0 * a.q.ldc + col / 2, *scales = a.q.scales + row0 * a.q.lds + col / kMxBlock;
       const int there = (int)min((int64_t)R, a.rows - row0), rows = stored ? there : 0;
-      RowRandom<T> random;
+      RowRandom<V> random;
       uint32_t kept = 0;  // of the lanes of a block, one keeps the scale of each row
       const auto one = [&](auto index) {
         constexpr int i = decltype(index)::value;
         if (RANDOM && i >= there) return;
         // opaque, or the compiler would convert the values of all rows first, past the registers
-        if constexpr (COLS && RANDOM && std::is_same_v<T, _Float16>) asm volatile("" : "+v"(x.v[i].x), "+v"(x.v[i].y), "+v"(x.v[i].z), "+v"(x.v[i].w));
+        if constexpr (COLS && RANDOM && std::is_same_v<T, _Float16>) {
+#pragma unroll
+          for (int k = 0; k < x.kWords; ++k) asm volatile("" : "+v"(x.v[i].w[k]));
+        }
         if (RANDOM && i % random.kRows == 0) random.make(a, row0 + i, col);
-        const uint32_t s = mx_scale(mx_max_bits<T>(mx_max_of_lanes<kLanes>(mx_max16<T>(x.v[i]))));
-        const uint32_t c = RANDOM ? row_codes_random<T>(x.v[i], s, random.w[i % random.kRows][0], random.w[i % random.kRows][1])
-                                  : mx_codes16<T>(x.v[i], s);
+        const uint32_t s = mx_scale(mx_max_bits<T>(mx_max_of_lanes<kLanes>(mx_max16<T>(whole(x.v[i])))));
+        const uint32_t c = RANDOM ? row_codes_random(x.v[i], s, random.w[i % random.kRows][0], random.w[i % random.kRows][1])
+                                  : row_codes(x.v[i], s);
         if (i < rows) {
-          if constexpr (sizeof(T) == 4) *reinterpret_cast<uint16_t*>(codes + i * a.q.ldc) = (uint16_t)c;
+          if constexpr (V == 4) *reinterpret_cast<uint16_t*>(codes + i * a.q.ldc) = (uint16_t)c;
           else *reinterpret_cast<uint32_t*>(codes + i * a.q.ldc) = c;
         }
         if (lane % kLanes == i % kLanes) kept = s;
@@ -198,8 +244,8 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
         const int k = e * (int)sizeof(T) / 4, part = e * (int)sizeof(T) % 4;  // word and byte of value e
         // opaque, or what was made of the values for the rows would be kept for here
 #pragma unroll
-        for (int i = 0; i < R; ++i) asm volatile("" : "+v"(reinterpret_cast<uint32_t*>(&x.v[i])[k]));
-        const auto word = [&](int i) { return reinterpret_cast<const uint32_t*>(&x.v[i])[k]; };
+        for (int i = 0; i < R; ++i) asm volatile("" : "+v"(x.v[i].w[k]));
+        const auto word = [&](int i) { return x.v[i].w[k]; };
         // two rows' values of the column as a pair, for 16-bit types
         const auto pair = [&](int i) { return __builtin_amdgcn_perm(word(i + 1), word(i), part ? 0x07060302u : 0x05040100u); };
         uint32_t most = 0;
@@ -222,7 +268,7 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
             const U4 r = stream_block(a.seed, kMx4Cols, a.epoch, (uint64_t)((col + e) * per16 + 2 * block + h));
             float f[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) f[i] = value_at<T>(x.v[16 * h + i], e);
+            for (int i = 0; i < 16; ++i) f[i] = value_at(x.v[16 * h + i], e);
             c[2 * h] = codes_random<8>(f, s, r.x, r.y);
             c[2 * h + 1] = codes_random<8>(f + 8, s, r.z, r.w);
           }
@@ -344,32 +390,45 @@ int launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols,
                         const MxView* qt, int32_t rounding, uint64_t seed, uint32_t epoch, int cus, hipStream_t s) {
   return with_type(type, [&](auto t) {
     using T = decltype(t);
-    constexpr int64_t kWidth = 64 * 16 / sizeof(T);  // columns of a tile
-    QuantArgs a{x, rows, cols, ldx, q ? *q : MxView{}, qt ? *qt : MxView{}, seed, epoch, 0, 0};
-    // the padding is written too: of the columns where rows are quantized, of the rows where columns are
-    a.across = ((q ? mx_groups(cols) * kMxGroup : cols) + kWidth - 1) / kWidth;
-    const bool random = rounding == HALP_ROUND_STOCHASTIC;
-    // Rows alone: one row a wave where there are so few that the waves count, else eight.
-    const int height = qt ? 32 : rows <= 1024 ? 1 : 8;
-    a.tiles = a.across * ((rows + 4 * height - 1) / (4 * height));
-    // Both forms of a tile by one workgroup, so that x is read once; by two, side by side, where that leaves no CU without
-    // one: 300 x 4096 in bf16 8.3 us instead of 10.9, stochastically 15.0 instead of 22.0
-    const dim3 grid(grid_of(a.tiles), q && qt && a.tiles <= cus ? 2 : 1);
-    const auto launch = [&](auto with_rows, auto with_cols, auto is_random, auto tall) {
-      hipLaunchKernelGGL((quantize_tiles<T, decltype(with_rows)::value, decltype(with_cols)::value, decltype(is_random)::value,
-                                         decltype(tall)::value>), grid, dim3(256), 0, s, a);
+    const auto by_width = [&](auto values) {  // of a lane
+      constexpr int V = decltype(values)::value;
+      constexpr int64_t kWidth = 64 * V;  // columns of a tile
+      QuantArgs a{x, rows, cols, ldx, q ? *q : MxView{}, qt ? *qt : MxView{}, seed, epoch, 0, 0};
+      // the padding is written too: of the columns where rows are quantized, of the rows where columns are
+      a.across = ((q ? mx_groups(cols) * kMxGroup : cols) + kWidth - 1) / kWidth;
+      const bool random = rounding == HALP_ROUND_STOCHASTIC;
+      // Rows alone: one row a wave where there are so few that the waves count, else eight.
+      const int height = qt ? 32 : rows <= 1024 ? 1 : 8;
+      a.tiles = a.across * ((rows + 4 * height - 1) / (4 * height));
+      // Both forms of a tile by one workgroup, so that x is read once; by two, side by side, where that leaves no CU without
+      // one (300 x 4096 in bf16 8.3 us instead of 10.9, stochastically 15.0 instead of 22.0, with eight values a lane)
+      const dim3 grid(grid_of(a.tiles), q && qt && a.tiles <= cus ? 2 : 1);
+      const auto launch = [&](auto with_rows, auto with_cols, auto is_random, auto tall) {
+        hipLaunchKernelGGL((quantize_tiles<T, decltype(with_rows)::value, decltype(with_cols)::value, decltype(is_random)::value,
+                                           decltype(tall)::value, V>), grid, dim3(256), 0, s, a);
+      };
+      const std::true_type yes{};
+      const std::false_type no{};
+      const auto by_form = [&](auto is_random) {
+        if (q && qt) launch(yes, yes, is_random, std::integral_constant<int, 32>{});
+        else if (qt) launch(no, yes, is_random, std::integral_constant<int, 32>{});
+        else if constexpr (V == 16 / sizeof(T)) {
+          if (height == 8) launch(yes, no, is_random, std::integral_constant<int, 8>{});
+          else launch(yes, no, is_random, std::integral_constant<int, 1>{});
+        }
+      };
+      if (random) by_form(yes);
+      else by_form(no);
+      return hip_ok(hipGetLastError());
     };
-    const std::true_type yes{};
-    const std::false_type no{};
-    const auto by_form = [&](auto is_random) {
-      if (q && qt) launch(yes, yes, is_random, std::integral_constant<int, 32>{});
-      else if (qt) launch(no, yes, is_random, std::integral_constant<int, 32>{});
-      else if (height == 8) launch(yes, no, is_random, std::integral_constant<int, 8>{});
-      else launch(yes, no, is_random, std::integral_constant<int, 1>{});
-    };
-    if (random) by_form(yes);
-    else by_form(no);
-    return hip_ok(hipGetLastError());
+    // Four values of 16 bits a lane instead of eight, twice as many tiles, where tiles are few.  In bf16, us with eight and
+    // four: columns of 300 x 4096 7.4 / 5.6, 4096 x 4096 13.3 / 13.0, 8192 x 4096 22.9 / 23.2; both forms of 300 x 4096
+    // 8.6 / 8.1 and 2000 x 4096 11.6 / 12.1, stochastically 15.0 / 12.9 and 17.9 / 17.0, of 3000 x 4096 23.0 / 27.7.
+    if constexpr (sizeof(T) == 2) {
+      const int64_t tiles = ((rows + 127) / 128) * ((cols + 511) / 512);
+      if (qt && tiles <= (!q ? cus : rounding == HALP_ROUND_STOCHASTIC ? cus / 2 : cus / 4)) return by_width(std::integral_constant<int, 4>{});
+    }
+    return by_width(std::integral_constant<int, 16 / sizeof(T)>{});
   });
 }
 

@@ -131,6 +131,26 @@ def test_rows_shorter_than_a_load(rows, cols, ld, stochastic, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("cols,ld", [(1, 1), (3, 3), (7, 9), (33, 33)])
+def test_many_short_rows(cols, ld, stochastic, dtype):
+    """Tiles of which there are many, whose rows end within a lane's values and whose last rows end the memory."""
+    rows = 33_101
+    g = torch.Generator("cuda").manual_seed(cols)
+    held = torch.empty((rows - 1) * ld + cols, device="cuda", dtype=dtype).as_strided((rows, cols), (ld, 1))
+    held.copy_(torch.randn(rows, cols, generator=g, device="cuda"))
+    how = dict(rounding=int(stochastic), seed=8, epoch=3)
+    (q, *a), (qt, *b), (one, *c) = _empty(rows, cols), _empty(cols, rows), _empty(rows, cols)
+    hp.mx4_quantize(held, q, qt, **how)
+    _check(qt, *b, *mx4.quantize(held.double().cpu().numpy().T, stochastic, epoch=3, seed=8, purpose=7))
+    hp.mx4_quantize(held, one, **how)
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+    if not stochastic:
+        codes, scales = mx4.quantize(held[-70:].double().cpu().numpy())
+        assert np.array_equal(a[0][rows - 70:rows].cpu().numpy(), mx4.pack(codes)) and np.array_equal(a[1][rows - 70:rows].cpu().numpy(), scales)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("stochastic", [False, True])
 def test_special_values(stochastic, dtype):
     """Every number of the grid, the ties, their neighbours and signed zeros at scales over the whole range of the
     type; subnormals; the largest numbers; blocks with infinities and NaN."""
