@@ -410,7 +410,7 @@ int halp_mx4_dequantize(const halp_mx4* q, void* out, int32_t type, int64_t ldo,
  * halp_mx4_product_workspace bytes, products with few tiles and a long K are cut along K and their parts joined in a
  * fixed order; without it the same products run uncut and end in another rounding.  Calls that
  * overlap in time must not share it.  c must not overlap the operands or the workspace.
- * ceil(M / 64) ceil(N / 64) >= 2^25 - 3: HALP_ERR_UNSUPPORTED.                                 */
+ * ceil(M / 64) ceil(N / 64) >= 2^25 - 3: HALP_ERR_UNSUPPORTED, from both calls.                */
 int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type, int64_t ldc, int32_t accumulate,
                      void* workspace, int64_t workspace_bytes, void* stream);
 int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes); /* on the current device */

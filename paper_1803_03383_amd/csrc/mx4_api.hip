@@ -12,7 +12,7 @@ constexpr int64_t kMost = int64_t(1) << 31;
 // A launch holds fewer than 2^32 threads.  A product's tiles have 2 threads for each of their 64, 128 or 256 rows; A by B
 // tiles of 64 are at most (A + 1) / 2 by (B + 1) / 2 of 128 and (A + 3) / 4 by (B + 3) / 4 of 256, and with A = 1, where
 // these weigh most, 512 (B + 3) / 4 < 2^32 where B < 2^25 - 3.
-constexpr int64_t kMostTiles = (int64_t(1) << 25) - 3;
+bool too_many_tiles(int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64) >= (int64_t(1) << 25) - 3; }
 
 int check_matrix(const halp_mx4& q) {
   if (q.rows < 0 || q.cols < 0 || q.rows >= kMost || q.cols >= (int64_t(1) << 24)) return HALP_ERR_INVALID;
@@ -87,7 +87,7 @@ int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type
   if (a->cols != b->cols || (accumulate != 0 && accumulate != 1) || workspace_bytes < 0) return HALP_ERR_INVALID;
   if (accumulate && type != HALP_TYPE_F32) return HALP_ERR_UNSUPPORTED;
   if (workspace && !aligned(workspace, 16)) return HALP_ERR_ALIGN;
-  if (((a->rows + 63) / 64) * ((b->rows + 63) / 64) >= kMostTiles) return HALP_ERR_UNSUPPORTED;
+  if (too_many_tiles(a->rows, b->rows)) return HALP_ERR_UNSUPPORTED;
   if (a->rows == 0 || b->rows == 0) return HALP_OK;
   int cus = 0;
   if ((rc = count_cus(&cus)) != HALP_OK) return rc;
@@ -98,6 +98,7 @@ int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type
 int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes) {
   if (!bytes) return HALP_ERR_NULL;
   if (M < 0 || N < 0 || K < 0 || M >= kMost || N >= kMost || K >= kMost) return HALP_ERR_INVALID;
+  if (too_many_tiles(M, N)) return HALP_ERR_UNSUPPORTED;
   int cus = 0;
   if (const int rc = count_cus(&cus)) return rc;
   *bytes = mx4_product_workspace(M, N, K, cus);

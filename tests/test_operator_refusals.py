@@ -70,6 +70,7 @@ def test_product():
     most = 64 * (2 ** 25 - 4)  # rows of 64 by 2^25 - 4 tiles, the most of a launch
     for a, b in ((1, most + 1), (most + 1, 1), (65, most // 2 + 1), (2 ** 31 - 1, 2 ** 31 - 1)):
         assert product(a=_mx(rows=a), b=_mx(rows=b), ldc=2 ** 31) == hp.ERR_UNSUPPORTED
+        assert L.halp_mx4_product_workspace(a, b, 200, C.byref(C.c_int64())) == hp.ERR_UNSUPPORTED
     assert L.halp_mx4_product_workspace(1, 1, 1, None) == hp.ERR_NULL
     n = C.c_int64()
     assert L.halp_mx4_product_workspace(-1, 1, 1, C.byref(n)) == hp.ERR_INVALID
