@@ -248,10 +248,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_tiles(ProductArgs a) {
   for (int m = 0; m < FM; ++m) products(std::integral_constant<int, 3>{}, m);
 
   // 32 rows at a time through LDS (each wave its own part), so that rows leave in 16-byte pieces, whole lines
-  // together: straight from the accumulators a line would be written 8 bytes at a time.
+  // together: straight from the accumulators a line would be written 8 bytes at a time.  The rows lie where the last stage's
+  // codes were: every wave must have its fragments of them, not only have asked for them.  The last products may stand
+  // behind the barrier, and the compiler waits for their fragments no earlier, so the barrier does.
   constexpr int kPer = 16 / sizeof(T), kRow = FN * 32 + kPer, kPieces = FN * 32 / kPer;  // elements, pieces a row
   static_assert(WM * WN * 32 * kRow * sizeof(T) <= sizeof lds, "");
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   T* own = reinterpret_cast<T*>(lds) + wave * 32 * kRow;
 #pragma unroll
   for (int m = 0; m < FM; ++m) {
