@@ -43,16 +43,16 @@ using LPtr = __attribute__((address_space(3))) void*;
 // 64 times 16 bytes from base + off (a lane's own, 32 bits) to LDS at `to` (bytes, a multiple of 1024 past the wave's
 // start) and up, lane after lane.  Issued by hand: the compiler takes the builtin for a store to all of LDS
 // and would have every later LDS read wait for it.  Complete after s_waitcnt vmcnt(0).  on: ~0 or 0, all lanes or none, so that
-// a load can be left out without a branch, which would part the products around it.  All lanes are active.
+// a load can be left out without a branch, which would part the products around it.  All lanes are active.  m0 holds `to`.
 __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t off, uint32_t to, uint32_t on) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
-               ::"s"(to), "v"(off), "s"(base), "s"(on));
+  asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+               ::"{m0}"(to), "v"(off), "s"(base), "s"(on));
 }
 
 // the same of 64 times 4 bytes, 256 in all
 __device__ __forceinline__ void word_to_lds(const uint8_t* base, uint32_t off, uint32_t to, uint32_t on) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1"
-               ::"s"(to), "v"(off), "s"(base), "s"(on));
+  asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1"
+               ::"{m0}"(to), "v"(off), "s"(base), "s"(on));
 }
 
 // a pointer that is the same in every lane, in scalar registers
