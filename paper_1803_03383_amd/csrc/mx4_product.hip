@@ -8,10 +8,9 @@
 // so that its scales of the stage are one word and the instruction picks the byte.  16-byte pieces of
 // a row are permuted in LDS (piece p of row r lies at p ^ r / 2 % 8), so that the 16 rows that are read at once
 // cover every bank once; the permutation is made on the source address.
-#include <cmath>
-
 #include "halp_internal.hpp"
 #include "mx4.hpp"
+#include "mx4_plan.hpp"
 
 namespace halp {
 namespace {
@@ -314,56 +313,13 @@ __global__ __launch_bounds__(256) void join_cuts(JoinArgs a) {
 
 }  // namespace
 
-namespace {
-
-// How a product is made: the edge of its tiles (256, 128, 64: one, two, three workgroups to a CU) and the parts that K is
-// cut in.  Small tiles fill the CUs where there are few, at the price of more reads; parts cost a pass over
-// them.  The choice is the least of an estimate in microseconds fitted to timings of 21 sizes on this GPU (its choices take
-// 1 % longer than the best there, the worst 10 %): a stage takes 1.9 with 256-tiles on every CU (1.0 with a few: the
-// power limit), 0.77 and 1.27 with one and two 128-tiles on a CU, 0.42 to 0.8 with one to three 64-tiles; beginning and
-// ending a tile 10.5, 4 and 3.4.  On both sides of its borders (measured, us): 4096 x 4096 x 2048 28 / 29 / 44 with
-// 256 / 128 / 64, 4096 x 2048 x 4096 31 / 26 / 42, 300 x 4096 x 4096 27 / 13.3 / 13.0; 1000 x 784 x 60000 with 128 in
-// 1, 2, 4, 8, 16 parts 152, 82, 50, 49, 57.
-struct Plan {
-  int tile, cuts;
-};
-
-Plan plan(int64_t M, int64_t N, int64_t K, int cus) {
-  const int64_t stages = (mx_groups(K) + 1) / 2;
-  const auto stage_us = [&](int tile, double per_cu) {  // workgroups per CU
-    const int n = (int)std::ceil(per_cu);
-    if (tile == 256) return 1.0 + 0.9 * (per_cu < 1 ? per_cu : 1);
-    if (tile == 128) return n == 1 ? 0.77 : 1.27;
-    return n == 1 ? 0.42 : n == 2 ? 0.61 : 0.8;
-  };
-  Plan best{128, 1};
-  double least = 1e300;
-  for (int tile = 256, most = 1; tile >= 64; tile /= 2, ++most)
-    for (int cuts = 1; cuts == 1 || (cuts <= 16 && stages / cuts >= 4); cuts *= 2) {
-      const double blocks = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * cuts / cus;  // per CU
-      const double ends = tile == 256 ? 10.5 : tile == 128 ? 4 : 3.4, full = std::floor(blocks / most), rest = blocks - full * most;
-      const double length = (double)((stages + cuts - 1) / cuts);
-      double us = full * (length * stage_us(tile, most) + ends);
-      if (rest > 0) us += length * stage_us(tile, rest) + ends;
-      if (cuts > 1) us += 4.4 + (double)cuts * M * N * 8 / 8.5e6;
-      if (us < least) least = us, best = Plan{tile, cuts};
-    }
-  return best;
-}
-
-int64_t parts_stride(int64_t N) { return (N + 3) / 4 * 4; }
-
-}  // namespace
-
 int64_t mx4_product_workspace(int64_t M, int64_t N, int64_t K, int cus) {
-  const Plan p = plan(M, N, K, cus);
-  return p.cuts > 1 ? sizeof(float) * p.cuts * M * parts_stride(N) : 0;
+  return plan_workspace(M, N, product_plan(M, N, K, cus, kMostCuts));
 }
 
 int launch_mx4_product(const MxView& a, const MxView& b, void* c, int32_t type, int64_t ldc, bool accumulate,
                        void* workspace, int64_t workspace_bytes, int cus, hipStream_t s) {
-  Plan p = plan(a.rows, b.rows, a.cols, cus);
-  if (workspace_bytes < mx4_product_workspace(a.rows, b.rows, a.cols, cus)) p.cuts = 1;
+  const ProductPlan p = product_plan_within(a.rows, b.rows, a.cols, cus, workspace_bytes);
   const int64_t t = p.tile, tm = (a.rows + t - 1) / t, tn = (b.rows + t - 1) / t;
   const auto tiles = [&](auto kind, void* out, int64_t ld, bool add) {
     using T = decltype(kind);
