@@ -455,7 +455,8 @@ typedef struct {
   int64_t step;           /* t, 1 <= t < 2^32                                                  */
   const int64_t* step_at; /* DEVICE, or NULL: t is read there instead (a step captured into a
                              graph; the caller counts it up).  A t out of range skips the step */
-  const float* lr_at;     /* DEVICE, or NULL: lr is read there instead                         */
+  const float* lr_at;     /* DEVICE, or NULL: lr is read there instead.  One that is negative or not finite
+                             skips the step                                                     */
   const float* grad_scale; /* DEVICE, or NULL for 1: s.  Where it is not finite the step is
                              skipped: every tensor is left as it was                           */
 } halp_adamw_args;

@@ -506,8 +506,8 @@ class AdamW:
     def step(self, step=1, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=None, step_at=None,
              lr_at=None, stream=None):
         """One step.  step counts from 1; step_at (int64) and lr_at (float32), one-element GPU tensors, take the place of
-        step and lr where given; grad_scale (float32, one element) scales the gradients and skips the step where it
-        is not finite."""
+        step and lr where given; grad_scale (float32, one element) scales the gradients.  Where one of the three is out
+        of its range on the GPU (step_at from 1 to 2^32 - 1, lr_at finite and not negative, grad_scale finite), the step is skipped."""
         at = []
         for name, t, dtype in (("step_at", step_at, _torch.int64), ("lr_at", lr_at, _torch.float32),
                                ("grad_scale", grad_scale, _torch.float32)):

@@ -139,8 +139,9 @@ __global__ __launch_bounds__(kThreads, BITS8 ? 4 : 2) void adamw_step(StepArgs a
   const float scale = a.grad_scale ? *a.grad_scale : 1.f;
   if (!(fabsf(scale) < __builtin_inff())) return;
   const int64_t step = a.step_at ? *a.step_at : a.step;
-  if (step < 1 || step >= (int64_t(1) << 32)) return;
-  const double lr = a.lr_at ? (double)*a.lr_at : a.lr;
+  const float lr_at = a.lr_at ? *a.lr_at : 0.f;
+  if (step < 1 || step >= (int64_t(1) << 32) || !(lr_at >= 0 && lr_at < __builtin_inff())) return;
+  const double lr = a.lr_at ? (double)lr_at : a.lr;
   const float keep = (float)(1 - lr * a.decay), rate = (float)(lr / (1 - power(a.beta1, step))),
               root = (float)(1 / sqrt(1 - power(a.beta2, step))), b1 = (float)a.beta1, b2 = (float)a.beta2,
               n1 = (float)(1 - a.beta1), n2 = (float)(1 - a.beta2);

@@ -1,0 +1,32 @@
+"""Calls of the 4-bit microscaled operators and of AdamW with values at the ends of what they take, on the GPU."""
+import pytest
+import torch
+
+import paper_1803_03383_amd as hp
+
+pytestmark = pytest.mark.gpu
+
+
+def _adamw(bits, n=5000):
+    g = torch.Generator("cuda").manual_seed(bits)
+    t = {k: torch.randn(n, generator=g, device="cuda") for k in ("p", "g")}
+    if bits == 32:
+        t |= {k: torch.rand(n, generator=g, device="cuda") * 1e-3 for k in ("m", "v")}
+    else:
+        t |= {k: torch.randint(0, 100, (n,), generator=g, device="cuda", dtype=torch.uint8) for k in ("m", "v")}
+        t |= {k: torch.full(((n + 31) // 32,), 117, device="cuda", dtype=torch.uint8) for k in ("m_scale", "v_scale")}
+    t["copy"] = torch.full((n,), 3.0, device="cuda", dtype=torch.bfloat16)
+    return t, hp.AdamW([t], state_bits=bits, seed=3)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_rate_in_device_memory_that_the_host_would_refuse_skips_the_step(bits):
+    t, plan = _adamw(bits)
+    before = {k: v.clone() for k, v in t.items()}
+    for bad in (float("nan"), float("inf"), -float("inf"), -1e-3):
+        plan.step(1, lr_at=torch.tensor([bad], device="cuda"))
+        assert all(torch.equal(v, before[k]) for k, v in t.items()), bad
+    for lr in (0.0, -0.0, 1e-3):  # zero is a rate: it moves the moments and not p
+        plan.step(1, lr_at=torch.tensor([lr], device="cuda"))
+        assert torch.equal(t["p"], before["p"]) == (lr == 0)
+        assert not torch.equal(t["m"], before["m"])
