@@ -368,6 +368,11 @@ def _same_device(t, *others):
     return dev
 
 
+def _count(n):
+    """A number that the library takes in 32 of 64 bits; -1, which it refuses, in place of what ctypes would cut to 64."""
+    return n if 0 <= n < 2 ** 32 else -1
+
+
 def _run(name, dev, stream, *args):
     """Calls the library with device `dev` current, on the stream given or on that device's current one."""
     torch = _load_torch()
@@ -416,7 +421,7 @@ def mx4_quantize(x, q=None, qt=None, rounding=ROUND_NEAREST, seed=0, epoch=0, st
     """x [rows, cols] into q (Mx4 of its rows) and qt (Mx4 of its transpose), whichever are given."""
     dev = _same_device(x, q and q.codes, qt and qt.codes)
     _run("halp_mx4_quantize", dev, stream, x.data_ptr(), _type(x, "x"), x.shape[0], x.shape[-1], _matrix(x, "x"),
-         q and q.ref, qt and qt.ref, rounding, seed & (2 ** 64 - 1), epoch)
+         q and q.ref, qt and qt.ref, rounding, seed & (2 ** 64 - 1), _count(epoch))
 
 
 def mx4_dequantize(q, out, stream=None):
@@ -519,7 +524,7 @@ class AdamW:
             if _same_device(t) != self._dev:
                 raise ValueError(f"{name}: on {t.device}, the tensors on cuda:{self._dev}")
             at.append(t.data_ptr())
-        a = AdamWArgs(lr, beta1, beta2, eps, weight_decay, step, *at)
+        a = AdamWArgs(lr, beta1, beta2, eps, weight_decay, _count(step), *at)
         _run("halp_adamw_step", self._dev, stream, self._h, C.byref(a))
 
     def grad_norm(self, max_norm, out, stream=None):

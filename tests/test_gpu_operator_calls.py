@@ -30,3 +30,18 @@ def test_a_rate_in_device_memory_that_the_host_would_refuse_skips_the_step(bits)
         plan.step(1, lr_at=torch.tensor([lr], device="cuda"))
         assert torch.equal(t["p"], before["p"]) == (lr == 0)
         assert not torch.equal(t["m"], before["m"])
+
+
+@pytest.mark.parametrize("number", [-1, 2 ** 32, 2 ** 63, 2 ** 64, 2 ** 64 + 1, -2 ** 64 + 1])
+def test_numbers_past_the_range_of_the_streams_are_refused(number):
+    """Also those whose low 64 bits are within it."""
+    x, q = torch.ones(3, 40, device="cuda"), hp.mx4_empty(3, 40)
+    q.codes.fill_(7)
+    with pytest.raises(hp.HalpError) as e:
+        hp.mx4_quantize(x, q, rounding=hp.ROUND_STOCHASTIC, epoch=number)
+    assert e.value.code == hp.ERR_INVALID and (q.codes == 7).all()
+    t, plan = _adamw(32, 100)
+    before = t["p"].clone()
+    with pytest.raises(hp.HalpError) as e:
+        plan.step(number)
+    assert e.value.code == hp.ERR_INVALID and torch.equal(t["p"], before)
