@@ -397,8 +397,9 @@ int halp_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, i
                       const halp_mx4* qt, int32_t rounding, uint64_t seed, int64_t epoch, void* stream);
 
 /* The values that q stands for, into out (DEVICE, [rows][ldo], ldo >= cols, elements of `type`):
- * exact in fp32 and bf16 (below 2^-126: rounded to the type); fp16 rounds, and overflows to
- * infinity.                                                                                   */
+ * exact in fp32 and bf16 between 2^-126 and 2^128.  Below they are rounded to the type; from 2^128 on they
+ * are infinity.  The largest numbers of these types come to that: past 3 2^126 the next value is 4 2^126 (to
+ * the nearest from 3.5 2^126 on).  fp16 rounds, and overflows to infinity.                     */
 int halp_mx4_dequantize(const halp_mx4* q, void* out, int32_t type, int64_t ldo, void* stream);
 
 /* c[M][N] = a[M][K] b[N][K]^T, and added to c where accumulate is 1 (fp32 only); M = a->rows,

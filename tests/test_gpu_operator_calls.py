@@ -1,8 +1,10 @@
 """Calls of the 4-bit microscaled operators and of AdamW with values at the ends of what they take, on the GPU."""
+import numpy as np
 import pytest
 import torch
 
 import paper_1803_03383_amd as hp
+from oracle import mx4
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +47,18 @@ def test_numbers_past_the_range_of_the_streams_are_refused(number):
     with pytest.raises(hp.HalpError) as e:
         plan.step(number)
     assert e.value.code == hp.ERR_INVALID and torch.equal(t["p"], before)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("stochastic", [False, True])
+def test_the_largest_numbers_are_read_back_as_the_format_has_them(stochastic, dtype):
+    """No value is clamped, so that one between 3 2^126 and 4 2^126 comes to either: the latter is past fp32 and bf16."""
+    most = torch.finfo(dtype).max
+    x = torch.tensor([most, -most, 3.5 * 2.0 ** 126, 3.75 * 2.0 ** 126, 3.25 * 2.0 ** 126, 3 * 2.0 ** 126, 2.0 ** 126, 1.0] * 16, device="cuda").to(dtype)[None]
+    q, back = hp.mx4_empty(*x.shape), torch.empty_like(x)
+    hp.mx4_quantize(x, q, rounding=int(stochastic), seed=1)
+    hp.mx4_dequantize(q, back)
+    want = mx4.values(*mx4.quantize(x.double().cpu().numpy(), stochastic, purpose=6, seed=1))
+    assert set(np.abs(want[0, ::8])) <= {3 * 2.0 ** 126, 2.0 ** 128} and 2.0 ** 128 in want
+    want[np.abs(want) >= 2.0 ** 128] *= np.inf
+    assert np.array_equal(back.double().cpu().numpy(), want)
