@@ -417,8 +417,8 @@ int halp_mx4_product(const halp_mx4* a, const halp_mx4* b, void* c, int32_t type
 int halp_mx4_product_workspace(int64_t M, int64_t N, int64_t K, int64_t* bytes); /* on the current device */
 
 /* y[M][N] = Q(x)[M][K] w[N][K]^T for 0 <= M <= 16 rows of x in `xtype`, quantized to the nearest on the
- * way (the values halp_mx4_quantize gives): a served token's product in one launch (two or more where the
- * rows hold more than about 100 000 values together).  Larger M, or K > 131072: HALP_ERR_UNSUPPORTED,
+ * way (the values halp_mx4_quantize gives): a served token's product in one launch (two or more where LDS does not
+ * hold the rows: up to 239 616 values together it does).  Larger M, or K > 131072: HALP_ERR_UNSUPPORTED,
  * quantize x and take halp_mx4_product.  y must not overlap x or w.                           */
 int halp_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, const halp_mx4* w, void* y,
                          int32_t ytype, int64_t ldy, void* stream);
@@ -435,7 +435,8 @@ int halp_mx4_row_product(const void* x, int32_t xtype, int64_t M, int64_t ldx, c
  * the largest of the block allows.  They are rounded stochastically, so that the small
  * changes that beta2 makes are not lost: element e of tensor i takes word e % 4 of block e / 4 of
  * purpose 8 of the stream of seed + i at epoch t, the low half for m and the high half for v;
- * p is updated from m and v before that rounding.  A block whose m (or v) is not finite
+ * p is updated from m and v before that rounding.  The root of v and the reciprocal of the
+ * denominator are within a step of fp32 each, the other operations rounded to the nearest.  A block whose m (or v) is not finite
  * gets s = 255 and reads as NaN.                                                              */
 typedef struct halp_adamw halp_adamw; /* opaque, library-owned */
 
@@ -463,7 +464,8 @@ typedef struct {
 } halp_adamw_args;
 
 /* The plan of a list of tensors: copies the list to the current device (the structs need not
- * outlive the call, the tensors do).  Tensors must not overlap; count >= 1.  state_bits 8 or 32.
+ * outlive the call, the tensors do).  It holds their addresses: tensors that move, gradients allocated anew among
+ * them, need a new one.  It outlives the graphs that its steps are captured into.  Tensors must not overlap; count >= 1.  state_bits 8 or 32.
  * Every pointer is aligned to its element.  Tensors whose p, g, m, v and copy are aligned to
  * four elements run fastest.                                                                 */
 int halp_adamw_create(halp_adamw** out, const halp_adamw_tensor* tensors, int64_t count, int32_t state_bits,
@@ -473,8 +475,9 @@ int halp_adamw_destroy(halp_adamw* h);
 /* One step of every tensor.  A handle keeps nothing between steps but its list.               */
 int halp_adamw_step(halp_adamw* h, const halp_adamw_args* args, void* stream);
 
-/* out[0] = the 2-norm of all gradients, out[1] = min(1, max_norm / out[0]), the grad_scale that
- * clips to it (1 for a norm of 0; NaN where the norm is not finite, so that the step is skipped).
+/* out[0] = the 2-norm of all gradients, out[1] = min(1, max_norm / norm), the grad_scale that
+ * clips to it (1 for a norm of 0; NaN where a gradient is not finite, so that the step is skipped).  A norm past
+ * fp32 is infinite in out[0] and clipped all the same: out[1] comes from its 64 bits.
  * Sums in 64 bits, joined in a fixed order, through workspace of the handle: calls on one handle that
  * overlap in time race.                                                                       */
 int halp_adamw_grad_norm(halp_adamw* h, double max_norm, float* out, void* stream);

@@ -62,3 +62,17 @@ def test_the_largest_numbers_are_read_back_as_the_format_has_them(stochastic, dt
     assert set(np.abs(want[0, ::8])) <= {3 * 2.0 ** 126, 2.0 ** 128} and 2.0 ** 128 in want
     want[np.abs(want) >= 2.0 ** 128] *= np.inf
     assert np.array_equal(back.double().cpu().numpy(), want)
+
+
+def test_a_norm_past_fp32_is_clipped():
+    """Finite gradients whose norm is not an fp32 number: the scale is that of the norm in 64 bits, within half a step."""
+    t, plan = _adamw(32, 5000)
+    t["g"].fill_(3e38)
+    out = torch.empty(2, device="cuda")
+    plan.grad_norm(1e30, out)
+    g = float(np.float32(3e38))
+    want = 1e30 / (g * 5000 ** 0.5)
+    assert float(out[0]) == float("inf") and abs(float(out[1]) / want - 1) <= 1.01 * 2.0 ** -24
+    plan.step(1, grad_scale=out[1:])
+    # m = 0.1 g', beside which 0.9 of what it was is nothing: the roundings of the scale, g', 1 - beta1, their product and the sum
+    assert ((t["m"].double() / (0.1 * g * want) - 1).abs() <= 5 * 1.01 * 2.0 ** -24).all()
