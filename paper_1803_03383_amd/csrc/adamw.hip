@@ -131,9 +131,12 @@ __device__ __forceinline__ float fast_sqrt(float v) {
   return small ? r * 0x1p-48f : r;
 }
 
-// Four consecutive elements per lane, eight lanes to a block of 8-bit states.  Bound by memory with 32-bit states (5.3 TB/s
-// of 240 M elements, where a copy of 2 GB runs at 4.9); with 8-bit states the random blocks and the conversions take about
-// as long as the memory (4.1 TB/s of 100 M, and 5.3 with gradients in fp32 and a copy, in the same time).
+// Four consecutive elements per lane, eight lanes to a block of 8-bit states.  Bound by memory with 32-bit states: 240 M
+// elements at 5.3 TB/s where steps follow each other, 5.0 behind the norm of the same gradients (a copy of 2 GB runs at
+// 4.9).  With 8-bit states the random blocks and the conversions take about as long as the memory: 100 M at 4.3 TB/s in a row of
+// steps, 4.7 among other work, and 5.1 with gradients in fp32 and a copy.  Those kernels are held to 128 registers, four waves
+// a SIMD, and spill two to five of them; with three waves and nothing spilled the same steps take 324 us in place of 325
+// and 360 in place of 355.
 template <typename G, typename C, bool BITS8>
 __global__ __launch_bounds__(kThreads, BITS8 ? 4 : 2) void adamw_step(StepArgs a) {
   const float scale = a.grad_scale ? *a.grad_scale : 1.f;

@@ -197,7 +197,8 @@ __global__ __launch_bounds__(256, 2) void quantize_tiles(QuantArgs a) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   // The column blocks of the four waves meet here: blocks by value, lane and wave, the wave's place permuted so that lanes
   // write to all banks (8192 x 8192 fp16 both ways 63 us without it and 54 with).  Not where they are rounded
-  // stochastically: the arithmetic bounds that (100 us either way).
+  // stochastically: the arithmetic bounds that.  In us without and with it, 8192 x 8192 fp16 both ways 79 / 83 and columns alone
+  // 52 / 46, 8192 x 4096 bf16 38 / 39 and 22 / 22, 4095 x 5000 fp32 40.1 / 40.5 and 21.1 / 21.4.
   constexpr bool kMeet = COLS && !RANDOM;
   __shared__ uint4 out[kMeet ? 64 * kV * 4 : 1];
   __shared__ __align__(4) uint8_t out_scales[kMeet ? 64 * kV * 4 : 4];

@@ -1,11 +1,13 @@
 // Products of a few rows with an MX4 matrix: y = Q(x) w^T, the rows quantized on the way.
 //
-// Bound by reading w once.  A workgroup quantizes the rows into LDS while its first loads of w are on their way, and
-// then takes units of w, one after another: 16 rows for each `split` of its waves, which share K between them
-// and join their sums in LDS in the order of the waves.  A wave reads w in chunks of four groups (512 values)
-// of 16 rows, two ahead of the one it multiplies, across the units' borders.  Within a chunk lane quarter q
-// takes the four blocks of group q: its codes are 64 bytes in a row, its four scales one word, and
-// v_mfma_scale_f32_16x16x128_f8f6f4 multiplies block j of the four groups.
+// Bound by trips to memory, one after another.  A workgroup quantizes the rows into LDS and then takes units of w, one
+// after another: 16 rows for each `split` of its waves, which share K between them and join their sums in LDS in the order of
+// the waves.  A wave reads w in chunks of four groups (512 values) of 16 rows, across the units' borders.  Its first two are asked for
+// before the rows, and each further one before the products of the chunk two before it; but as this is compiled a
+// chunk has arrived before the next load is asked for (its word of scales is masked as soon as it is there, and chunks
+// change registers), so that what is on the way at a time is one chunk a wave: 13 rows times 11000 x 5000 take 12 us, 29 MB of w
+// at the rate of a copy 6.  Within a chunk lane quarter q takes the four blocks of group q: its codes are 64 bytes in a row,
+// its four scales one word, and v_mfma_scale_f32_16x16x128_f8f6f4 multiplies block j of the four groups.
 #include "halp_internal.hpp"
 #include "mx4.hpp"
 
@@ -149,7 +151,7 @@ __global__ __launch_bounds__(64 * kWaves) void row_product(RowArgs a) {
     if (a.split > 1) {
       v4f32* to = sums + parity * waves * 64;
       to[wave * 64 + lane] = acc;
-      // the sums only: loads of w stay in flight
+      // the sums only: nothing in memory is waited for
       lds_barrier();
       if (part) continue;
       for (int k = 1; k < a.split; ++k) acc += to[(wave + k) * 64 + lane];
